@@ -443,6 +443,144 @@ int fp8rl_attention_decode_bf16kv(const uint16_t* q, const uint16_t* k_cache, co
                                   int64_t head_dim, int64_t max_seq_len, float sm_scale, uint16_t* out,
                                   void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * Causal attention over whole prompts: packed sequences of different lengths, grouped query heads
+ * (query head h reads kv head h / (q_heads / kv_heads)).  Token i of sequence b is row
+ * cu_seqlens[b] + i of q, k, v and out, and attends to tokens 0 .. i of its own sequence:
+ *   out[i][h] = sum_{t <= i} p_t v_t / sum_{t <= i} p_t,   p_t = e^(sm_scale * q[i][h] . k[t])
+ * The scores are bf16 x bf16 -> fp32, the softmax fp32; p_t / p_max is rounded to bf16 for the
+ * product with the bf16 values (fp32 accumulation), the output once to bf16.
+ *
+ * q    DEVICE bf16 [total][ld_q]: query head h of a token at columns 128 h ..
+ * k, v DEVICE bf16 [total][ld_k], [total][ld_v]: kv head h at columns 128 h ..
+ *      (row pitches in elements: column ranges of one fused qkv output will do)
+ * out  DEVICE bf16 [total][ld_out], as q; must not overlap the inputs
+ * cu_seqlens  DEVICE int32 [batch + 1], non-decreasing, cu_seqlens[0] >= 0 and the last one <=
+ *      total (precondition; offsets are clamped into [0, total], so that nothing outside the rows is
+ *      touched).  Sequences may be empty; rows before the first offset or from the last one on are
+ *      read by no sequence and written by none.
+ * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; total * q_heads / 128 + batch * kv_heads < 2^23
+ * (else FP8RL_ERR_UNSUPPORTED_SHAPE).  total == 0 or batch == 0 is a no-op.
+ * Alignment: q, k, v, out 16-byte, every ld a multiple of 8, cu_seqlens 4-byte.
+ */
+int fp8rl_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t* k, int64_t ld_k, const uint16_t* v,
+                                int64_t ld_v, const int32_t* cu_seqlens, int64_t batch, int64_t total, int64_t q_heads,
+                                int64_t kv_heads, int64_t head_dim, float sm_scale, uint16_t* out, int64_t ld_out,
+                                void* stream);
+
+/*
+ * The same for new tokens of sequences whose keys and values, theirs included, are in the paged FP8
+ * cache (written by fp8rl_kv_cache_write_fp8): a chunk of a prompt, drafted tokens, single decode
+ * tokens, mixed as they come.  Rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of q are the last n of
+ * the seq_lens[b] tokens of sequence b: row i of them attends to the cache's tokens
+ * 0 .. seq_lens[b] - n + i.  A row in front of the first token (n > seq_lens[b]) gives 0.
+ * Keys and values are code * (*k_scale), code * (*v_scale); p_t / p_max is rounded to fp16 (the codes
+ * are exact there).
+ *
+ * k_cache, v_cache, num_blocks, block_table, max_blocks, k_scale, v_scale: as for
+ * fp8rl_attention_decode_fp8kv (a block id outside the cache is clamped into it); seq_lens DEVICE
+ * int32 [batch], tokens past max_seq_len are ignored, max_blocks * 16 >= max_seq_len.
+ * workspace    caller-lent device memory of fp8rl_attention_prompt_workspace_size(batch, total,
+ *              q_heads, kv_heads, max_seq_len) bytes, 16-byte aligned, not shared by calls (or
+ *              captured graphs) that may overlap; may be NULL where that is 0 (few rows over long
+ *              sequences are split along the keys, which takes a record per row and split)
+ * The rest, alignment and limits as above; max_seq_len < 2^30.
+ */
+int64_t fp8rl_attention_prompt_workspace_size(int64_t batch, int64_t total, int64_t q_heads, int64_t kv_heads,
+                                              int64_t max_seq_len);
+
+int fp8rl_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                 int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                 const int32_t* seq_lens, const int32_t* cu_seqlens, int64_t batch, int64_t total,
+                                 int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_seq_len,
+                                 const float* k_scale, const float* v_scale, float sm_scale, uint16_t* out,
+                                 int64_t ld_out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Decode attention, as fp8rl_attention_decode_fp8kv, for a batch whose sequences share long prefixes
+ * (the samples drawn from one prompt): the keys and values of a prefix are read once for all
+ * sequences of its group.
+ *
+ * group_offsets  DEVICE int32 [num_groups + 1], non-decreasing: sequences group_offsets[g] ..
+ *                group_offsets[g + 1] - 1 are group g's; groups may be empty, and a sequence of no
+ *                group is attended to on its own
+ * prefix_lens    DEVICE int32 [num_groups]: the first prefix_lens[g] tokens of the group's sequences
+ *                are the same (precondition), rounded down to whole 16-token blocks here, and to no
+ *                more than max_prefix_len or the length of the group's first sequence, whose row of
+ *                the block table names the shared blocks (the other rows' entries for them are not
+ *                read).  A sequence shorter than the prefix attends to its own length of it.
+ * max_prefix_len 0 .. max_seq_len
+ * workspace      fp8rl_attention_decode_shared_workspace_size(batch, num_groups, q_heads, kv_heads,
+ *                max_prefix_len, max_seq_len) bytes, 16-byte aligned, not shared by calls (or captured
+ *                graphs) that may overlap
+ * num_groups 1 .. 65535; everything else as for fp8rl_attention_decode_fp8kv.
+ */
+int64_t fp8rl_attention_decode_shared_workspace_size(int64_t batch, int64_t num_groups, int64_t q_heads,
+                                                     int64_t kv_heads, int64_t max_prefix_len, int64_t max_seq_len);
+
+int fp8rl_attention_decode_shared_fp8kv(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                        int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                        const int32_t* seq_lens, int64_t batch, const int32_t* group_offsets,
+                                        const int32_t* prefix_lens, int64_t num_groups, int64_t max_prefix_len,
+                                        int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_seq_len,
+                                        const float* k_scale, const float* v_scale, float sm_scale, uint16_t* out,
+                                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Pages of the cache.  A block table row names a sequence's 16-token blocks; block_refs counts, for
+ * each block, the rows that name it, so that sequences can share blocks.  All arrays are the
+ * caller's, on the device; which blocks are free is for the caller to know (those of count 0).
+ *
+ * caches       HOST array of num_caches >= 1 DEVICE pointers, read during the call only: every key and
+ *              value cache (of all layers) that the block table goes for, each num_blocks blocks of
+ *              block_bytes (a multiple of 16; kv_heads * 2048 for the FP8 caches), 16-byte aligned
+ * block_table  DEVICE int32 [rows][max_blocks]; seq_lens DEVICE int32 [rows] (a length counts as at
+ *              most max_blocks * 16); block_refs DEVICE int32 [num_blocks]
+ * num_blocks, rows, max_blocks < 2^31 (rows * max_blocks may pass it); num_caches <= 65536; count <
+ * 2^24 (else FP8RL_ERR_UNSUPPORTED_SHAPE).  count == 0 is a no-op.
+ *
+ * fp8rl_kv_copy_blocks: block dst[i] of every cache becomes a copy of block src[i] (DEVICE int32
+ * [count]).  Pairs with an index outside [0, num_blocks) are skipped.  No block may be both a source
+ * and a destination, and none a destination twice.
+ *
+ * fp8rl_kv_fork_sequences: for each i < count (parents, children, new_blocks DEVICE int32 [count]), row
+ * children[i] gets the tokens of row parents[i]: its whole blocks are shared (their counts go up by
+ * one), its last block, where it is partly filled, is copied to block new_blocks[i] in every cache
+ * (whose count goes up by one, from the caller's 0; not used where the parent ends with a whole
+ * block), and seq_lens[children[i]] becomes the parent's.  Entries of the row behind that stay, and
+ * what the row named before is not given back: free it first.  A fork with a row outside
+ * [0, rows), of a row to itself, or that needs a block outside the cache is skipped.  No row may be
+ * both a parent and a child, or a child twice, in one call.
+ *
+ * fp8rl_kv_free_sequences: the counts of the blocks of the rows sequences[0 .. count - 1] go down by
+ * one, the rows' lengths become 0 (a row named twice is freed once); rows outside [0, rows) are
+ * skipped.
+ *
+ * fp8rl_kv_compact: with L the number of blocks in use (count > 0), written to *live (DEVICE int32),
+ * moves the blocks in use at L and above into the free ones below L: the k-th lowest free one takes
+ * the k-th highest in use.  Their contents move in every cache, their counts with them, and the
+ * entries of every row (up to its length) follow.  Blocks from L on are free afterwards; below L a
+ * block keeps its place and contents.  workspace: fp8rl_kv_compact_workspace_size(num_blocks) bytes, 4-byte
+ * aligned, not shared by calls that may overlap.
+ */
+int fp8rl_kv_copy_blocks(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,
+                         const int32_t* src, const int32_t* dst, int64_t count, void* stream);
+
+int fp8rl_kv_fork_sequences(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,
+                            int32_t* block_table, int64_t rows, int64_t max_blocks, int32_t* seq_lens,
+                            int32_t* block_refs, const int32_t* parents, const int32_t* children,
+                            const int32_t* new_blocks, int64_t count, void* stream);
+
+int fp8rl_kv_free_sequences(const int32_t* block_table, int64_t rows, int64_t max_blocks, int32_t* seq_lens,
+                            int32_t* block_refs, int64_t num_blocks, const int32_t* sequences, int64_t count,
+                            void* stream);
+
+int64_t fp8rl_kv_compact_workspace_size(int64_t num_blocks);
+
+int fp8rl_kv_compact(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,
+                     int32_t* block_table, int64_t rows, int64_t max_blocks, const int32_t* seq_lens,
+                     int32_t* block_refs, int32_t* live, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Human-readable name of a status code (static string, never NULL). */
 const char* fp8rl_status_string(int status);
 

@@ -30,6 +30,10 @@ __all__ = [
     "fp8rl_tis_workspace_size", "fp8rl_tis_weights_kl",
     "fp8rl_kv_calibrate_scale", "fp8rl_kv_cache_write_fp8", "fp8rl_attention_decode_workspace_size",
     "fp8rl_attention_decode_fp8kv", "fp8rl_attention_decode_bf16kv",
+    "fp8rl_attention_prompt_bf16", "fp8rl_attention_prompt_workspace_size", "fp8rl_attention_prompt_fp8kv",
+    "fp8rl_attention_decode_shared_workspace_size", "fp8rl_attention_decode_shared_fp8kv",
+    "fp8rl_kv_copy_blocks", "fp8rl_kv_fork_sequences", "fp8rl_kv_free_sequences",
+    "fp8rl_kv_compact_workspace_size", "fp8rl_kv_compact",
     "fp8rl_status_string", "fp8rl_version",
     "quant_weight_block128", "quant_act_token_group128", "gemm_w8a8_block",
     "grouped_gemm_w8a8_block", "silu_mul_quant_group128", "gather_rows_fp8", "linear_w8a8",
@@ -81,6 +85,14 @@ def _load():
         "fp8rl_attention_decode_fp8kv": [P, P, P, I, P, I, P, I, I, I, I, I, P, P, ctypes.c_float, P, P, I, P],
         "fp8rl_attention_decode_bf16kv": [P, P, P, I, P, I, P, I, I, I, I, I, ctypes.c_float, P, P, I, P],
         "fp8rl_gather_rows_fp8": [P, I, P, I, I, P, I, I, P, I, P, I, P],
+        "fp8rl_attention_prompt_bf16": [P, I, P, I, P, I, P, I, I, I, I, I, ctypes.c_float, P, I, P],
+        "fp8rl_attention_prompt_fp8kv": [P, I, P, P, I, P, I, P, P, I, I, I, I, I, I, P, P, ctypes.c_float, P, I, P, I, P],
+        "fp8rl_attention_decode_shared_fp8kv": [P, P, P, I, P, I, P, I, P, P, I, I, I, I, I, I, P, P, ctypes.c_float, P, P,
+                                                I, P],
+        "fp8rl_kv_copy_blocks": [P, I, I, I, P, P, I, P],
+        "fp8rl_kv_fork_sequences": [P, I, I, I, P, I, I, P, P, P, P, P, I, P],
+        "fp8rl_kv_free_sequences": [P, I, I, P, P, I, P, I, P],
+        "fp8rl_kv_compact": [P, I, I, I, P, I, I, P, P, P, P, I, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -94,6 +106,12 @@ def _load():
     lib.fp8rl_kv_calibrate_workspace_size.restype = ctypes.c_int64
     lib.fp8rl_attention_decode_workspace_size.argtypes = [I, I, I, I]
     lib.fp8rl_attention_decode_workspace_size.restype = ctypes.c_int64
+    lib.fp8rl_attention_prompt_workspace_size.argtypes = [I, I, I, I, I]
+    lib.fp8rl_attention_prompt_workspace_size.restype = ctypes.c_int64
+    lib.fp8rl_attention_decode_shared_workspace_size.argtypes = [I, I, I, I, I, I]
+    lib.fp8rl_attention_decode_shared_workspace_size.restype = ctypes.c_int64
+    lib.fp8rl_kv_compact_workspace_size.argtypes = [I]
+    lib.fp8rl_kv_compact_workspace_size.restype = ctypes.c_int64
     lib.fp8rl_gemm_w8a8_block_workspace_size.argtypes = [I, I, I]
     lib.fp8rl_gemm_w8a8_block_workspace_size.restype = ctypes.c_int64
     lib.fp8rl_status_string.argtypes = [ctypes.c_int]
@@ -621,6 +639,243 @@ def fp8rl_attention_decode_bf16kv(q, k_cache, v_cache, block_table, seq_lens, ma
         raise TypeError("bf16 caches expected")
     return _attention("fp8rl_attention_decode_bf16kv", q, k_cache, v_cache, block_table, seq_lens, max_seq_len,
                       sm_scale, [], out, workspace, stream)
+
+
+def _head_rows(x: torch.Tensor, what: str):
+    """Row pitch of a bf16 [tokens][heads][128] tensor whose heads lie side by side."""
+    if x.dtype != torch.bfloat16 or x.dim() != 3:
+        raise TypeError(f"{what} must be bfloat16 [tokens][heads][head_dim]")
+    t, h, d = x.shape
+    if t > 0 and h > 0 and ((d > 1 and x.stride(2) != 1) or (h > 1 and x.stride(1) != d)):
+        raise ValueError(f"the heads of a token of {what} must lie side by side")
+    return x.stride(0) if t > 1 else h * d
+
+
+def _here(*ts):
+    """One HIP device for all, and the current one: kernels start there, on its current stream."""
+    _dev(*ts)
+    if ts[0].get_device() != torch._C._cuda_getDevice():
+        raise ValueError("fp8rl tensors must live on the current device")
+
+
+def _i32(x: torch.Tensor, n, what: str):
+    if x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous() or (n is not None and x.numel() != n):
+        raise ValueError(f"{what} must be contiguous int32 [{'n' if n is None else n}]")
+
+
+def _paged(k_cache, v_cache, block_table):
+    """Checked FP8 caches and block table: (k, v, num_blocks, kv_heads)."""
+    k_cache, v_cache = _u8(k_cache), _u8(v_cache)
+    if k_cache.dim() < 2 or not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("the caches must be contiguous [num_blocks][kv_heads][..]")
+    if k_cache.shape[:2] != v_cache.shape[:2] or k_cache.numel() != v_cache.numel() or \
+            k_cache.numel() != k_cache.shape[0] * k_cache.shape[1] * 2048:
+        raise ValueError("the caches must hold 16 x 128 codes per block and kv head")
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+        raise ValueError("block_table must be contiguous int32 [batch][max_blocks]")
+    return k_cache, v_cache, k_cache.shape[0], k_cache.shape[1]
+
+
+def _scale1(*scales):
+    for s in scales:
+        if s.dtype != torch.float32 or s.numel() != 1:
+            raise ValueError("k_scale and v_scale must be fp32 [1]")
+
+
+def _out_rows(out, q):
+    if out is None:
+        return torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    return out
+
+
+def _workspace(workspace, need: int, device):
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace
+
+
+def fp8rl_attention_prompt_bf16(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                                sm_scale: float, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention over packed prompts: q bf16 [T][q_heads][128], k and v [T][kv_heads][128] (any row
+    pitch: slices of one fused qkv output will do), sequence b in rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1
+    (device int32 [batch + 1]); returns bf16 [T][q_heads][128], rows of no sequence unwritten."""
+    name = "fp8rl_attention_prompt_bf16"
+    ld_q, ld_k, ld_v = _head_rows(q, "q"), _head_rows(k, "k"), _head_rows(v, "v")
+    total, q_heads, dim = q.shape
+    if k.shape != v.shape or k.shape[0] != total or k.shape[2] != dim:
+        raise ValueError("k and v must be [T][kv_heads][head_dim] of q's tokens")
+    _i32(cu_seqlens, None, "cu_seqlens")
+    if cu_seqlens.numel() < 1:
+        raise ValueError("cu_seqlens must have batch + 1 entries")
+    out = _out_rows(out, q)
+    ld_out = _head_rows(out, "out")
+    _here(q, k, v, cu_seqlens, out)
+    st = load().fp8rl_attention_prompt_bf16(q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+                                            cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, total, q_heads, k.shape[1], dim,
+                                            float(sm_scale), out.data_ptr(), ld_out, _stream(stream))
+    _check(name, st)
+    return out
+
+
+def fp8rl_attention_prompt_workspace_size(batch: int, total: int, q_heads: int, kv_heads: int, max_seq_len: int) -> int:
+    return int(load().fp8rl_attention_prompt_workspace_size(batch, total, q_heads, kv_heads, max_seq_len))
+
+
+def fp8rl_attention_prompt_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                                 seq_lens: torch.Tensor, cu_seqlens: torch.Tensor, max_seq_len: int, k_scale: torch.Tensor,
+                                 v_scale: torch.Tensor, sm_scale: float, out: torch.Tensor | None = None,
+                                 workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention of new tokens against the paged FP8 caches, which hold them already: rows cu_seqlens[b] ..
+    of q (bf16 [T][q_heads][128]) are the last of sequence b's seq_lens[b] tokens; returns bf16 [T][q_heads][128]."""
+    name = "fp8rl_attention_prompt_fp8kv"
+    ld_q = _head_rows(q, "q")
+    total, q_heads, dim = q.shape
+    k_cache, v_cache, num_blocks, kv_heads = _paged(k_cache, v_cache, block_table)
+    batch = block_table.shape[0]
+    _i32(seq_lens, batch, "seq_lens")
+    _i32(cu_seqlens, batch + 1, "cu_seqlens")
+    _scale1(k_scale, v_scale)
+    out = _out_rows(out, q)
+    ld_out = _head_rows(out, "out")
+    need = fp8rl_attention_prompt_workspace_size(batch, total, q_heads, kv_heads, int(max_seq_len))
+    workspace = _workspace(workspace, need, q.device)
+    _here(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, out, workspace)
+    st = load().fp8rl_attention_prompt_fp8kv(q.data_ptr(), ld_q, k_cache.data_ptr(), v_cache.data_ptr(), num_blocks,
+                                             block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(),
+                                             cu_seqlens.data_ptr(), batch, total, q_heads, kv_heads, dim, int(max_seq_len),
+                                             k_scale.data_ptr(), v_scale.data_ptr(), float(sm_scale), out.data_ptr(),
+                                             ld_out, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                             _stream(stream))
+    _check(name, st)
+    return out
+
+
+def fp8rl_attention_decode_shared_workspace_size(batch: int, num_groups: int, q_heads: int, kv_heads: int,
+                                                 max_prefix_len: int, max_seq_len: int) -> int:
+    return int(load().fp8rl_attention_decode_shared_workspace_size(batch, num_groups, q_heads, kv_heads, max_prefix_len,
+                                                                   max_seq_len))
+
+
+def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                                        block_table: torch.Tensor, seq_lens: torch.Tensor, group_offsets: torch.Tensor,
+                                        prefix_lens: torch.Tensor, max_prefix_len: int, max_seq_len: int,
+                                        k_scale: torch.Tensor, v_scale: torch.Tensor, sm_scale: float,
+                                        out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                                        stream=None) -> torch.Tensor:
+    """Decode attention (fp8rl_attention_decode_fp8kv) of a batch in groups: sequences group_offsets[g] ..
+    group_offsets[g + 1] - 1 share their first prefix_lens[g] tokens, which are read once for all of them
+    (device int32 [groups + 1] and [groups]); returns bf16 [batch][q_heads][128]."""
+    name = "fp8rl_attention_decode_shared_fp8kv"
+    if q.dtype != torch.bfloat16 or q.dim() != 3 or not q.is_contiguous():
+        raise TypeError("q must be contiguous bfloat16 [batch][q_heads][head_dim]")
+    batch, q_heads, dim = q.shape
+    k_cache, v_cache, num_blocks, kv_heads = _paged(k_cache, v_cache, block_table)
+    if block_table.shape[0] != batch:
+        raise ValueError("block_table must have a row per sequence")
+    _i32(seq_lens, batch, "seq_lens")
+    _i32(prefix_lens, None, "prefix_lens")
+    groups = prefix_lens.numel()
+    _i32(group_offsets, groups + 1, "group_offsets")
+    _scale1(k_scale, v_scale)
+    out = _out_rows(out, q)
+    if out.dtype != torch.bfloat16 or not out.is_contiguous():
+        raise ValueError("out must be contiguous bfloat16")
+    need = fp8rl_attention_decode_shared_workspace_size(batch, groups, q_heads, kv_heads, int(max_prefix_len),
+                                                        int(max_seq_len))
+    workspace = _workspace(workspace, need, q.device)
+    _here(q, k_cache, v_cache, block_table, seq_lens, group_offsets, prefix_lens, k_scale, v_scale, out, workspace)
+    st = load().fp8rl_attention_decode_shared_fp8kv(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_blocks, block_table.data_ptr(), block_table.shape[1],
+        seq_lens.data_ptr(), batch, group_offsets.data_ptr(), prefix_lens.data_ptr(), groups, int(max_prefix_len), q_heads,
+        kv_heads, dim, int(max_seq_len), k_scale.data_ptr(), v_scale.data_ptr(), float(sm_scale), out.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(name, st)
+    return out
+
+
+def _cache_list(caches):
+    """(ctypes array of base pointers, count, bytes per block, blocks) of caches [num_blocks][..] of one block size."""
+    caches = list(caches)
+    if not caches:
+        raise ValueError("at least one cache")
+    blocks = caches[0].shape[0] if caches[0].dim() else 0
+    size = caches[0].numel() * caches[0].element_size()
+    for c in caches:
+        if not c.is_contiguous() or c.dim() < 2 or c.shape[0] != blocks or c.numel() * c.element_size() != size:
+            raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
+    return (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches]), len(caches), size // max(blocks, 1), blocks
+
+
+def _table(block_table, seq_lens, block_refs, blocks=None):
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+        raise ValueError("block_table must be contiguous int32 [rows][max_blocks]")
+    _i32(seq_lens, block_table.shape[0], "seq_lens")
+    _i32(block_refs, blocks, "block_refs")
+
+
+def fp8rl_kv_copy_blocks(caches, src: torch.Tensor, dst: torch.Tensor, stream=None):
+    """Block dst[i] of every cache (a list of tensors [num_blocks][..] of one block size: all layers' keys and values)
+    becomes a copy of block src[i]; src, dst device int32 [n], pairs outside the caches are skipped."""
+    ptrs, n, size, blocks = _cache_list(caches)
+    _i32(src, None, "src")
+    _i32(dst, src.numel(), "dst")
+    _here(*caches, src, dst)
+    _check("fp8rl_kv_copy_blocks", load().fp8rl_kv_copy_blocks(ptrs, n, size, blocks, src.data_ptr(), dst.data_ptr(),
+                                                               src.numel(), _stream(stream)))
+
+
+def fp8rl_kv_fork_sequences(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, block_refs: torch.Tensor,
+                            parents: torch.Tensor, children: torch.Tensor, new_blocks: torch.Tensor, stream=None):
+    """Row children[i] of the block table gets the tokens of row parents[i]: whole blocks shared (block_refs, int32
+    [num_blocks], goes up), a partly filled last block copied to block new_blocks[i] of every cache."""
+    ptrs, n, size, blocks = _cache_list(caches)
+    _table(block_table, seq_lens, block_refs, blocks)
+    _i32(parents, None, "parents")
+    _i32(children, parents.numel(), "children")
+    _i32(new_blocks, parents.numel(), "new_blocks")
+    _here(*caches, block_table, seq_lens, block_refs, parents, children, new_blocks)
+    _check("fp8rl_kv_fork_sequences", load().fp8rl_kv_fork_sequences(
+        ptrs, n, size, blocks, block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(),
+        block_refs.data_ptr(), parents.data_ptr(), children.data_ptr(), new_blocks.data_ptr(), parents.numel(),
+        _stream(stream)))
+
+
+def fp8rl_kv_free_sequences(block_table: torch.Tensor, seq_lens: torch.Tensor, block_refs: torch.Tensor,
+                            sequences: torch.Tensor, stream=None):
+    """The blocks of the rows `sequences` (device int32 [n]) count one row less, the rows' lengths become 0."""
+    _table(block_table, seq_lens, block_refs)
+    _i32(sequences, None, "sequences")
+    _here(block_table, seq_lens, block_refs, sequences)
+    _check("fp8rl_kv_free_sequences", load().fp8rl_kv_free_sequences(
+        block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(), block_refs.data_ptr(),
+        block_refs.numel(), sequences.data_ptr(), sequences.numel(), _stream(stream)))
+
+
+def fp8rl_kv_compact_workspace_size(num_blocks: int) -> int:
+    return int(load().fp8rl_kv_compact_workspace_size(num_blocks))
+
+
+def fp8rl_kv_compact(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, block_refs: torch.Tensor,
+                     live: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Moves the blocks in use (block_refs > 0) to the front of every cache, their counts and the block table's entries
+    with them; returns their number, int32 [1] on the device: the blocks from there on are free."""
+    ptrs, n, size, blocks = _cache_list(caches)
+    _table(block_table, seq_lens, block_refs, blocks)
+    dev = block_table.device
+    if live is None:
+        live = torch.empty(1, dtype=torch.int32, device=dev)
+    _i32(live, 1, "live")
+    workspace = _workspace(workspace, fp8rl_kv_compact_workspace_size(blocks), dev)
+    _here(*caches, block_table, seq_lens, block_refs, live, workspace)
+    _check("fp8rl_kv_compact", load().fp8rl_kv_compact(
+        ptrs, n, size, blocks, block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(),
+        block_refs.data_ptr(), live.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _stream(stream)))
+    return live
 
 
 # short aliases

@@ -4,24 +4,14 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "api_util.hpp"
 #include "fp8rl.h"
 #include "launch.hpp"
 
 namespace {
 
-constexpr int64_t kMaxDim = int64_t(1) << 31;   // per-dimension limit (32-bit tile indices)
-constexpr int64_t kMaxLd = int64_t(1) << 24;     // GEMM operand row pitch limit (32-bit in-tile DMA offsets)
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int hip_status(hipError_t e) { return e == hipSuccess ? FP8RL_OK : FP8RL_ERR_HIP; }
-
-hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
-
 // Validation shared by the dense GEMM entry points: an FP8RL_* error, FP8RL_OK for
 // a valid call with nothing to do, or kLaunch.
-constexpr int kLaunch = -1;
-
 int check_dense(const uint8_t* qa, int64_t lda, const float* sa, int64_t ld_sa, const uint8_t* qw, int64_t ldw,
                 const float* sw, const uint16_t* y, int64_t ldy, int64_t m, int64_t n, int64_t k) {
   if (m < 0 || n < 0 || k < 0) return FP8RL_ERR_INVALID_ARG;

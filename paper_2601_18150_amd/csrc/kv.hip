@@ -26,6 +26,7 @@
 
 #include <type_traits>
 
+#include "attn_merge.hpp"
 #include "common.hpp"
 #include "gemm_core.hpp"
 #include "launch.hpp"
@@ -36,11 +37,6 @@ namespace {
 constexpr int kDim = 128;          // head dimension
 constexpr int kPage = 16;          // tokens per cache block
 constexpr float kE4M3Max = 448.0f;
-// A running maximum before its first score: finite, so that scores of -inf (a query-key
-// product past the range of fp32) weigh exp(-inf) = 0 also where they are the first ones
-// seen, instead of exp(-inf + inf) = NaN; below or equal to every finite score.
-constexpr float kNoScore = -3.4028234663852886e38f;
-
 typedef __bf16 v8bf16_t __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf16_t __attribute__((ext_vector_type(2)));
 typedef __bf16 v4bf16_t __attribute__((ext_vector_type(4)));
@@ -311,15 +307,6 @@ __device__ __forceinline__ float max_over_rows(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Partial record per (sequence, kv head, split): o[G][128], then m[G], l[G],
-// padded to a multiple of 4 floats (16-byte aligned records).
-template <int kG>
-constexpr int partial_floats() { return kG * kDim + (2 * kG + 3) / 4 * 4; }
-template <int kG>
-constexpr int rec_m() { return kG * kDim; }
-template <int kG>
-constexpr int rec_l() { return kG * kDim + kG; }
-
 // Workgroup = 4 waves on one split of one (sequence, kv head): wave w attends over
 // pages w, w + 4, ... of the split's split_pages pages, and the four results are
 // combined in LDS at the end, so a split leaves one record (or, when the whole
@@ -383,8 +370,8 @@ __device__ __forceinline__ void attn_decode_split_of(
     const typename CacheElem<kFp8>::T* __restrict__ vcache, int64_t num_blocks,
     const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens, int max_seq_len,
     const float* __restrict__ k_scale, const float* __restrict__ v_scale, float sm_scale, int kv_heads,
-    int split_pages, int max_splits, float* __restrict__ partial, uint16_t* __restrict__ out,
-    uint8_t* lds) {
+    int first_page, int split_pages, int records, int first_record, bool direct, float* __restrict__ partial,
+    uint16_t* __restrict__ out, uint8_t* lds) {
   constexpr int kElem = kFp8 ? 1 : 2;
   constexpr int kHalf = AttnLds<kG, kFp8>::kHalf;
   constexpr int kDepth = kRingDepth;
@@ -398,7 +385,7 @@ __device__ __forceinline__ void attn_decode_split_of(
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
   const int g = lane >> 4, j = lane & 15;
-  const int p0 = split * split_pages;
+  const int p0 = first_page + split * split_pages;
   const int32_t* table = block_table + (int64_t)b * max_blocks;
   auto page_id = [&](int i) {                             // a bad entry reads a wrong page, never outside
     const int blk = table[min(p0 + wave + i * kWaves, max_blocks - 1)];
@@ -411,7 +398,7 @@ __device__ __forceinline__ void attn_decode_split_of(
   const int p1 = min((n + kPage - 1) / kPage, p0 + split_pages);
   uint16_t* orow = out + ((int64_t)b * kv_heads + kvh) * kG * kDim;
   if (p0 >= p1) {                                         // (uniform over the workgroup)
-    if (max_splits == 1)                                  // an empty sequence gives 0
+    if (direct)                                           // an empty sequence gives 0
       for (int i = threadIdx.x; i < kG * kDim / 2; i += 256) reinterpret_cast<uint32_t*>(orow)[i] = 0u;
     return;
   }
@@ -567,7 +554,7 @@ __device__ __forceinline__ void attn_decode_split_of(
     }
   }
   __syncthreads();
-  float* rec = partial + (((int64_t)b * kv_heads + kvh) * max_splits + split) * partial_floats<kG>();
+  float* rec = partial + (((int64_t)b * kv_heads + kvh) * records + first_record + split) * partial_floats<kG>();
   for (int e = threadIdx.x; e < kG * kDim / 2; e += 256) {
     const int head = e / (kDim / 2), d = 2 * (e % (kDim / 2));
     float mm = kNoScore;
@@ -586,7 +573,7 @@ __device__ __forceinline__ void attn_decode_split_of(
       a0 += c[head * kDim + d] * f[w];
       a1 += c[head * kDim + d + 1] * f[w];
     }
-    if (max_splits == 1) {                       // the whole sequence: the output itself
+    if (direct) {                                // the whole sequence: the output itself
       const float f = (v_scale ? v_scale[0] : 1.0f) / ls;
       reinterpret_cast<uint32_t*>(orow)[e] = f32_to_bf16_rne(a0 * f) | (f32_to_bf16_rne(a1 * f) << 16);
     } else {
@@ -608,69 +595,40 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_decode_kernel(
     int split_pages, int max_splits, float* __restrict__ partial, uint16_t* __restrict__ out) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[AttnLds<kG, kFp8>::kBytes];
   attn_decode_split_of<kG, kFp8>(q, kcache, vcache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale,
-                                 v_scale, sm_scale, kv_heads, split_pages, max_splits, partial, out, lds);
+                                 v_scale, sm_scale, kv_heads, 0, split_pages, max_splits, 0, max_splits == 1, partial,
+                                 out, lds);
 }
 
-// out[b][head][d] = bf16( v_scale * sum_s e^(m_s - M) o_s[d] / sum_s e^(m_s - M) l_s ),
-// one workgroup per (head, sequence): 32 lanes hold the head's dims, kMergeSets such
-// sets take the splits in turn (the records' loads are then independent of each other)
-// and are combined in LDS.  Empty sequences give 0.
-constexpr int kMergeSets = 4;
-
+// out[b][head] = the sequence's split records joined (attn_merge.hpp), one workgroup per (head,
+// sequence).  Empty sequences give 0.
 template <int kG>
 __global__ __launch_bounds__(32 * kMergeSets) void attn_merge_kernel(
     const float* __restrict__ partial, const int32_t* __restrict__ seq_lens, int max_seq_len,
     const float* __restrict__ v_scale, int kv_heads, int split_pages, int max_splits, uint16_t* __restrict__ out) {
-  __shared__ float red[kMergeSets][kDim + 2];
   const int head = blockIdx.x, b = blockIdx.y;
   const int kvh = head / kG, h = head % kG;
-  const int set = threadIdx.x >> 5, d = 4 * (threadIdx.x & 31);
   const int n = min(seq_lens[b], max_seq_len);
   const int ns = min(max_splits, (max(n, 0) + split_pages * kPage - 1) / (split_pages * kPage));
   const float* base = partial + ((int64_t)b * kv_heads + kvh) * max_splits * partial_floats<kG>();
-  float m = kNoScore, l = 0.0f;
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int s = set; s < ns; s += kMergeSets) {
-    const float* r = base + (int64_t)s * partial_floats<kG>();
-    const float ms = r[rec_m<kG>() + h], ls = r[rec_l<kG>() + h];
-    const float4 o = *reinterpret_cast<const float4*>(r + h * kDim + d);
-    const float mn = fmaxf(m, ms), f = expf(m - mn), w = expf(ms - mn);
-    l = l * f + ls * w;
-    a.x = a.x * f + o.x * w;
-    a.y = a.y * f + o.y * w;
-    a.z = a.z * f + o.z * w;
-    a.w = a.w * f + o.w * w;
-    m = mn;
-  }
-  *reinterpret_cast<float2*>(&red[set][d]) = make_float2(a.x, a.y);
-  *reinterpret_cast<float2*>(&red[set][d + 2]) = make_float2(a.z, a.w);
-  if (d == 0) {
-    red[set][kDim] = m;
-    red[set][kDim + 1] = l;
-  }
-  __syncthreads();
-  if (set != 0) return;
-  float mm = kNoScore, lsum = 0.0f;
-#pragma unroll
-  for (int s = 0; s < kMergeSets; ++s) mm = fmaxf(mm, red[s][kDim]);
-  a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int s = 0; s < kMergeSets; ++s) {
-    const float w = ns > 0 ? expf(red[s][kDim] - mm) : 0.0f;              // (a set without splits adds 0)
-    lsum += red[s][kDim + 1] * w;
-    a.x += red[s][d] * w;
-    a.y += red[s][d + 1] * w;
-    a.z += red[s][d + 2] * w;
-    a.w += red[s][d + 3] * w;
-  }
-  const float f = ns > 0 ? (v_scale ? v_scale[0] : 1.0f) / lsum : 0.0f;
-  uint2 o2;
-  o2.x = f32_to_bf16_rne(a.x * f) | (f32_to_bf16_rne(a.y * f) << 16);
-  o2.y = f32_to_bf16_rne(a.z * f) | (f32_to_bf16_rne(a.w * f) << 16);
-  uint32_t* orow = reinterpret_cast<uint32_t*>(out + ((int64_t)b * kv_heads * kG + head) * kDim + d);
-  orow[0] = o2.x;                                  // (out is 4-byte aligned)
-  orow[1] = o2.y;
+  merge_records<kG>(base, ns, ns, 0, h, v_scale, out + ((int64_t)b * kv_heads * kG + head) * kDim);
+}
+
+// One layer of a batch whose sequences have a first part attended to elsewhere: workgroup (kv
+// head, sequence, split) takes its share of the pages from first_page[b] on, divided evenly over
+// the records that the sequence has room for, and leaves record first_record + split.
+template <int kG>
+__global__ __launch_bounds__(kMfmaBounds) void attn_decode_rest_kernel(
+    const uint16_t* __restrict__ q, const uint8_t* __restrict__ kcache, const uint8_t* __restrict__ vcache,
+    int64_t num_blocks, const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens,
+    int max_seq_len, const float* __restrict__ k_scale, const float* __restrict__ v_scale, float sm_scale, int kv_heads,
+    const int32_t* __restrict__ first_page, int first_record, int records, float* __restrict__ partial) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[AttnLds<kG, true>::kBytes];
+  const int b = blockIdx.y;
+  const int from = max(first_page[b], 0);
+  const int per = rest_split_pages(min(seq_lens[b], max_seq_len), from, (int)gridDim.z);
+  attn_decode_split_of<kG, true>(q, kcache, vcache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale,
+                                 v_scale, sm_scale, kv_heads, from, per, records, first_record, false, partial, nullptr,
+                                 lds);
 }
 
 }  // namespace
@@ -792,6 +750,31 @@ hipError_t launch_attention_decode(const uint16_t* q, const void* k_cache, const
   FP8RL_ATTN(8)
 #undef FP8RL_ATTN
   return hipErrorInvalidValue;
+}
+
+// Records per (sequence, kv head) for the parts behind a shared prefix, as a decode step's splits.
+int attn_rest_records(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_seq_len) {
+  return attn_plan(batch, kv_heads, group, max_seq_len).splits;
+}
+
+hipError_t launch_attention_decode_rest(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                        int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                        const int32_t* seq_lens, int64_t batch, int64_t group, int64_t kv_heads,
+                                        int64_t max_seq_len, const float* k_scale, const float* v_scale, float sm_scale,
+                                        const int32_t* first_page, int first_record, int records, float* partial,
+                                        hipStream_t stream) {
+  const dim3 grid((unsigned)kv_heads, (unsigned)batch, (unsigned)(records - first_record));
+#define FP8RL_REST(G)                                                                                              \
+  if (group == G)                                                                                                  \
+    hipLaunchKernelGGL((attn_decode_rest_kernel<G>), grid, dim3(256), 0, stream, q, k_cache, v_cache, num_blocks,  \
+                       block_table, (int)max_blocks, seq_lens, (int)max_seq_len, k_scale, v_scale, sm_scale,       \
+                       (int)kv_heads, first_page, first_record, records, partial);
+  FP8RL_REST(1)
+  FP8RL_REST(2)
+  FP8RL_REST(4)
+  FP8RL_REST(8)
+#undef FP8RL_REST
+  return hipGetLastError();
 }
 
 }  // namespace fp8rl

@@ -120,4 +120,75 @@ hipError_t launch_attention_decode(const uint16_t* q, const void* k_cache, const
                                    int64_t max_seq_len, const float* k_scale, const float* v_scale, float sm_scale,
                                    uint16_t* out, float* partial, hipStream_t stream);
 
+// The decode kernel over the pages from first_page[b] on alone (FP8 cache): records first_record ..
+// records - 1 of each (sequence, kv head), nothing of `out`.
+int attn_rest_records(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_seq_len);
+
+hipError_t launch_attention_decode_rest(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                        int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                        const int32_t* seq_lens, int64_t batch, int64_t group, int64_t kv_heads,
+                                        int64_t max_seq_len, const float* k_scale, const float* v_scale, float sm_scale,
+                                        const int32_t* first_page, int first_record, int records, float* partial,
+                                        hipStream_t stream);
+
+// Attention of whole prompts and of chunks against the FP8 cache.
+struct PromptSplit {
+  int splits, split_keys;
+  int partial_floats;    // floats per (token, kv head, split) record
+};
+PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len);
+
+// workgroups per split
+int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads);
+
+hipError_t launch_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t* k, int64_t ld_k,
+                                        const uint16_t* v, int64_t ld_v, const int32_t* cu_seqlens, int64_t batch,
+                                        int64_t total, int64_t q_heads, int64_t kv_heads, float sm_scale, uint16_t* out,
+                                        int64_t ld_out, hipStream_t stream);
+
+hipError_t launch_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                         int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                         const int32_t* seq_lens, const int32_t* cu_seqlens, int64_t batch, int64_t total,
+                                         int64_t q_heads, int64_t kv_heads, int64_t max_seq_len, const float* k_scale,
+                                         const float* v_scale, float sm_scale, uint16_t* out, int64_t ld_out,
+                                         float* workspace, hipStream_t stream);
+
+// Decode attention of sequences that share prefixes.
+struct SharedSplit {
+  int prefix_records, split_keys;
+  int records;           // of a (sequence, kv head), the prefix's first
+  int partial_floats;
+};
+SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,
+                              int64_t max_seq_len);
+
+int64_t attn_shared_workgroups(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads);
+
+hipError_t launch_attention_decode_shared(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                          int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                          const int32_t* seq_lens, int64_t batch, const int32_t* group_offsets,
+                                          const int32_t* prefix_lens, int64_t groups, int64_t max_prefix_len,
+                                          int64_t q_heads, int64_t kv_heads, int64_t max_seq_len, const float* k_scale,
+                                          const float* v_scale, float sm_scale, uint16_t* out, float* workspace,
+                                          hipStream_t stream);
+
+// Pages of the caches of many layers (host array of their base pointers).
+constexpr int kCachesPerLaunch = 128;
+
+hipError_t launch_kv_copy_blocks(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,
+                                 const int32_t* src, const int32_t* dst, int64_t count, hipStream_t stream);
+
+hipError_t launch_kv_fork(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks, int32_t* table,
+                          int64_t rows, int64_t max_blocks, int32_t* seq_lens, int32_t* refs, const int32_t* parents,
+                          const int32_t* children, const int32_t* new_blocks, int64_t count, hipStream_t stream);
+
+hipError_t launch_kv_free(const int32_t* table, int64_t rows, int64_t max_blocks, int32_t* seq_lens, int32_t* refs,
+                          int64_t num_blocks, const int32_t* sequences, int64_t count, hipStream_t stream);
+
+int64_t kv_compact_workspace_words(int64_t num_blocks);
+
+hipError_t launch_kv_compact(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,
+                             int32_t* table, int64_t rows, int64_t max_blocks, const int32_t* seq_lens, int32_t* refs,
+                             int32_t* live, int32_t* workspace, hipStream_t stream);
+
 }  // namespace fp8rl

@@ -1,0 +1,192 @@
+// Causal attention over whole prompts (packed sequences of different lengths) and over chunks of
+// prompts against the paged FP8 cache; the tiles' arithmetic is in attn_core.hpp.
+//
+// A workgroup takes 128 rows of one (sequence, kv head): row r is token r / G of the sequence and
+// query head r % G of those that read the kv head, so that a prompt's short tiles at the diagonal
+// waste few keys, a chunk of a few tokens fills a tile G times better, and the group's heads read
+// each key once.  The sequences' tiles are counted from their offsets by every wave itself.  Grid
+// (kv head + kv_heads * tile, split): the tiles of a kv head share an XCD's L2 where kv_heads is a
+// multiple of eight; tiles with the most keys come first.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_core.hpp"
+#include "attn_merge.hpp"
+#include "launch.hpp"
+
+namespace fp8rl {
+namespace {
+
+struct PromptArgs {
+  const uint16_t* q;
+  int64_t ld_q;
+  const void* k;               // bf16 rows, or the FP8 key pages
+  int64_t ld_k;
+  const void* v;
+  int64_t ld_v;
+  int64_t num_blocks;          // (pages from here on)
+  const int32_t* block_table;
+  int max_blocks;
+  const int32_t* seq_lens;
+  int max_seq_len;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* cu_seqlens;
+  int batch, total, kv_heads, group_log2;
+  float sm_scale;
+  uint16_t* out;
+  int64_t ld_out;
+  int splits, split_keys;      // splits > 1: records instead of outputs
+  float* records;              // (token, kv head, split)
+  int32_t* counts;             // records of each token
+};
+
+template <bool kFp8>
+__global__ __launch_bounds__(kMfmaBounds) void attn_prompt_kernel(const PromptArgs p) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTileBytes];
+  const int kvh = blockIdx.x % p.kv_heads, tiles = gridDim.x / p.kv_heads;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  TileOf at;
+  if (!find_tile(p.cu_seqlens, p.batch, p.total, p.group_log2, tiles - 1 - (int)(blockIdx.x / p.kv_heads), at)) return;
+  const int group = 1 << p.group_log2;
+  const int len = kFp8 ? min(max(p.seq_lens[at.b], 0), p.max_seq_len) : at.n;
+  const int first = len - at.n;                         // position of the call's first token of the sequence
+  const int rows = at.n << p.group_log2, row0 = at.index * kAttnRows;
+  auto position = [&](int r) { return first + (min(r, rows - 1) >> p.group_log2); };
+  const int r = row0 + kRowsPerWave * wave + (lane & 31);
+  const int token = at.first + (min(r, rows - 1) >> p.group_log2);
+  const int head = kvh * group + (min(r, rows - 1) & (group - 1));
+  AttnRow row;
+  row.q = p.q + token * p.ld_q + head * kHeadDim;
+  row.limit = position(r);
+  row.wave_limit = position(row0 + kRowsPerWave * wave);
+  row.wave_last = position(row0 + kRowsPerWave * wave + kRowsPerWave - 1);
+  const int split = blockIdx.y;
+  const int begin = split * p.split_keys;
+  const int end = min(position(row0 + kAttnRows - 1) + 1, p.splits > 1 ? begin + p.split_keys : 0x7FFFFFFF);
+  if (p.splits > 1 && split == 0 && kvh == 0 && (r & (group - 1)) == 0 && r < rows && lane < 32)
+    p.counts[token] = row.limit < 0 ? 0 : row.limit / p.split_keys + 1;
+  if (begin >= end && p.splits > 1) return;
+
+  AttnAcc acc;
+  attn_init(acc);
+  bf16x8 q[8];
+  attn_load_q(row, q);
+  const float sscale = (kFp8 ? p.k_scale[0] : 1.0f) * p.sm_scale;
+  const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
+  uint8_t* keys = lds;
+  uint8_t* values = lds + kTileBytes;
+  for (int k0 = begin; k0 < end; k0 += kTileKeys) {
+    lds_barrier();                                      // every wave has read the tile before
+    if constexpr (kFp8) {
+      const PagedKv c8{static_cast<const uint8_t*>(p.k), static_cast<const uint8_t*>(p.v),
+                       p.block_table + (int64_t)at.b * p.max_blocks, p.num_blocks, p.max_blocks, p.kv_heads, kvh};
+      Fp8TileRegs f;
+      fetch_tile_fp8(c8, k0, len, f);
+      store_tile_fp8(f, k0, len, keys, values);
+    } else {
+      load_tile_bf16(static_cast<const uint16_t*>(p.k) + at.first * p.ld_k + kvh * kHeadDim, p.ld_k,
+                     static_cast<const uint16_t*>(p.v) + at.first * p.ld_v + kvh * kHeadDim, p.ld_v, k0, len, keys, values);
+      wait_vmcnt<0>();
+    }
+    lds_barrier();
+    if (k0 <= row.wave_last) attn_tile<kFp8>(acc, q, row, k0, c, keys, values);
+  }
+  const float l = half_sum(acc.l);
+  const bool valid = r < rows;
+  if (p.splits > 1) {
+    const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;
+    float* rec = p.records + (((int64_t)token * p.kv_heads + kvh) * p.splits + split) * floats;
+    const int h = head & (group - 1);
+    attn_store_f32(acc, rec + h * kHeadDim, valid);
+    if (valid && lane < 32) {
+      rec[group * kHeadDim + h] = fmaxf(acc.m * sscale, kNoScore);
+      rec[group * kHeadDim + group + h] = l;
+    }
+  } else {
+    const float f = l == 0.0f ? 0.0f : (kFp8 ? p.v_scale[0] : 1.0f) / l;   // no visible key: 0
+    attn_store_bf16(acc, f, p.out + token * p.ld_out + head * kHeadDim, valid);
+  }
+}
+
+// One workgroup per (query head, token): the token's records joined.
+template <int kG>
+__global__ __launch_bounds__(32 * kMergeSets) void attn_prompt_merge_kernel(const PromptArgs p) {
+  const int head = blockIdx.x, token = blockIdx.y + blockIdx.z * 32768;
+  const int lo = min(max(p.cu_seqlens[0], 0), p.total), hi = min(max(p.cu_seqlens[p.batch], 0), p.total);
+  if (token < lo || token >= hi) return;                 // rows of no sequence stay as they are
+  const int kvh = head / kG, h = head % kG;
+  const int ns = min(p.counts[token], p.splits);
+  const float* base = p.records + ((int64_t)token * p.kv_heads + kvh) * p.splits * partial_floats<kG>();
+  merge_records<kG>(base, ns, ns, 0, h, p.v_scale, p.out + token * p.ld_out + head * kHeadDim);
+}
+
+}  // namespace
+
+// Splits of the keys where the tiles alone are too few for the 512 workgroups that the chip holds:
+// as many as fill them, of at least 256 keys each.
+PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len) {
+  const int64_t wgs = attn_tile_bound(total * group, batch < total ? batch : total) * kv_heads;
+  int64_t splits = wgs > 0 ? (512 + wgs - 1) / wgs : 1;
+  int64_t keys = (max_seq_len + splits - 1) / splits;
+  keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;
+  if (keys < 256) keys = 256;
+  splits = (max_seq_len + keys - 1) / keys;
+  PromptSplit s;
+  s.splits = splits > 1 ? (int)splits : 1;
+  s.split_keys = (int)keys;
+  s.partial_floats = (int)(group * kHeadDim + (2 * group + 3) / 4 * 4);
+  return s;
+}
+
+int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads) {
+  return attn_tile_bound(total * group, batch < total ? batch : total) * kv_heads;
+}
+
+hipError_t launch_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t* k, int64_t ld_k,
+                                        const uint16_t* v, int64_t ld_v, const int32_t* cu_seqlens, int64_t batch,
+                                        int64_t total, int64_t q_heads, int64_t kv_heads, float sm_scale, uint16_t* out,
+                                        int64_t ld_out, hipStream_t stream) {
+  const int64_t group = q_heads / kv_heads;
+  PromptArgs p{};
+  p.q = q, p.ld_q = ld_q, p.k = k, p.ld_k = ld_k, p.v = v, p.ld_v = ld_v;
+  p.cu_seqlens = cu_seqlens, p.batch = (int)batch, p.total = (int)total, p.kv_heads = (int)kv_heads;
+  p.group_log2 = group_log2_of(group), p.sm_scale = sm_scale, p.out = out, p.ld_out = ld_out, p.splits = 1;
+  hipLaunchKernelGGL((attn_prompt_kernel<false>), dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads)),
+                     dim3(64 * kAttnWaves), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                         int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
+                                         const int32_t* seq_lens, const int32_t* cu_seqlens, int64_t batch, int64_t total,
+                                         int64_t q_heads, int64_t kv_heads, int64_t max_seq_len, const float* k_scale,
+                                         const float* v_scale, float sm_scale, uint16_t* out, int64_t ld_out,
+                                         float* workspace, hipStream_t stream) {
+  const int64_t group = q_heads / kv_heads;
+  const PromptSplit sp = attn_prompt_split(batch, total, group, kv_heads, max_seq_len);
+  PromptArgs p{};
+  p.q = q, p.ld_q = ld_q, p.k = k_cache, p.v = v_cache, p.num_blocks = num_blocks, p.block_table = block_table;
+  p.max_blocks = (int)max_blocks, p.seq_lens = seq_lens, p.max_seq_len = (int)max_seq_len;
+  p.k_scale = k_scale, p.v_scale = v_scale;
+  p.cu_seqlens = cu_seqlens, p.batch = (int)batch, p.total = (int)total, p.kv_heads = (int)kv_heads;
+  p.group_log2 = group_log2_of(group), p.sm_scale = sm_scale, p.out = out, p.ld_out = ld_out;
+  p.splits = sp.splits, p.split_keys = sp.split_keys;
+  p.records = workspace;
+  p.counts = reinterpret_cast<int32_t*>(workspace + total * kv_heads * sp.splits * sp.partial_floats);
+  hipLaunchKernelGGL((attn_prompt_kernel<true>),
+                     dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads), (unsigned)sp.splits),
+                     dim3(64 * kAttnWaves), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sp.splits == 1) return e;
+  const dim3 grid((unsigned)q_heads, (unsigned)(total < 32768 ? total : 32768), (unsigned)((total + 32767) / 32768));
+  const dim3 block(32 * kMergeSets);
+  if (group == 1) hipLaunchKernelGGL((attn_prompt_merge_kernel<1>), grid, block, 0, stream, p);
+  if (group == 2) hipLaunchKernelGGL((attn_prompt_merge_kernel<2>), grid, block, 0, stream, p);
+  if (group == 4) hipLaunchKernelGGL((attn_prompt_merge_kernel<4>), grid, block, 0, stream, p);
+  if (group == 8) hipLaunchKernelGGL((attn_prompt_merge_kernel<8>), grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace fp8rl
