@@ -55,6 +55,13 @@ __device__ __forceinline__ int value16_at(int step, int h, int dim) { return ((s
 // Offsets are clamped into [0, total], lengths below 0 count as 0.  false: behind the last tile.
 struct TileOf {
   int b, index, first, n;      // sequence, tile inside it, its first token, its tokens
+
+  __device__ __forceinline__ void to_scalars() {
+    b = __builtin_amdgcn_readfirstlane(b);
+    index = __builtin_amdgcn_readfirstlane(index);
+    first = __builtin_amdgcn_readfirstlane(first);
+    n = __builtin_amdgcn_readfirstlane(n);
+  }
 };
 
 __device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int total, int group_log2, int t, TileOf& out) {
@@ -89,8 +96,8 @@ inline int group_log2_of(int64_t g) { return g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 
 struct AttnRow {
   const uint16_t* q;       // its 128 query values
   int limit;               // last key it attends to (below the first key: none)
-  int wave_limit;          // the smallest limit of the wave's rows (no mask is needed up to it)
-  int wave_last;           // the largest (tiles behind it are skipped)
+  int all_limit;           // the smallest limit of the workgroup's rows (no mask is needed up to it)
+  int wave_last;           // the largest of the wave's (tiles behind it are skipped)
 };
 
 // Running state of a wave: lane L holds dims 8 (i / 4) + 4 (L / 32) + i % 4 of each 32 of row L % 32.
@@ -130,33 +137,92 @@ __device__ __forceinline__ void attn_load_q(const AttnRow& row, bf16x8 (&q)[8]) 
     q[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row.q + 16 * kk + 8 * h));
 }
 
-// One tile of keys k0 .. k0 + 63 in LDS.  c: the scores' factor times log2(e).
+// Where a lane's operands lie in a tile: keys of 16-dim step kk and 32-key half b at k[kk] + 32 b rows,
+// values of dims 32 d and 16-key step t at v[d] + 16 t rows (bf16), v[0] + value16_at(t, 0, 32 d) (f16).
 template <bool kF16Values>
-__device__ __forceinline__ void attn_tile(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int k0, float c,
-                                          const uint8_t* keys, const uint8_t* values) {
-  const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
-  f32x16 s[2];
+struct LaneOffsets {
+  int k[8];
+  int v[kF16Values ? 1 : 4];
+
+  __device__ __forceinline__ LaneOffsets() {
+    const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    s[b] = (f32x16)(0.0f);
+    for (int kk = 0; kk < 8; ++kk) k[kk] = key_at(j, 2 * kk + h);
+    if constexpr (kF16Values) {
+      v[0] = value16_at(0, h, j);
+    } else {
+      // ds_read_b64_tr_b16: of 16 lanes that point at four rows x 16 columns, lane i gets column i
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      const bf16x8 k = *reinterpret_cast<const bf16x8*>(keys + key_at(32 * b + j, 2 * kk + h));
-      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kk], s[b], 0, 0, 0);
+      for (int d = 0; d < 4; ++d)
+        v[d] = value_at(4 * h + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
     }
   }
-  if (k0 + kTileKeys - 1 > row.wave_limit) {              // (uniform over the wave)
+  __device__ __forceinline__ bf16x8 key(const uint8_t* keys, int i) const {     // i: 8 * half + step
+    return *reinterpret_cast<const bf16x8*>(keys + k[i & 7] + (i >> 3) * 32 * 256);
+  }
+  __device__ __forceinline__ uint4 value(const uint8_t* values, int i) const {  // i: 4 * step + d
+    if constexpr (kF16Values) {
+      return *reinterpret_cast<const uint4*>(values + v[0] + value16_at(i >> 2, 0, 32 * (i & 3)));
+    } else {
+      const uint8_t* at = values + v[i & 3] + (i >> 2) * 16 * 256;
+      const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at)));
+      const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * 256)));
+      return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  }
+};
+
+template <bool kF16Values>
+__device__ __forceinline__ f32x16 value_mfma(const uint4& v, const uint4& p, const f32x16& o) {
+  if constexpr (kF16Values)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, p), o, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), o, 0, 0, 0);
+}
+
+// Instruction order inside a block: sched<kind, n> asks for n of that kind next.
+constexpr int kSchedMfma = 0x8, kSchedLdsRead = 0x100;
+template <int kKind, int kCount>
+__device__ __forceinline__ void sched() { __builtin_amdgcn_sched_group_barrier(kKind, kCount, 0); }
+
+template <bool kF16Values>
+__device__ __forceinline__ uint32_t pack_p(float a, float b) {
+  return kF16Values ? pack_f16(a, b) : pack_bf16(a, b);
+}
+
+// Scores of the tile of keys k0 .. k0 + 63 in LDS, and P from them (in the type of the values), in
+// the order of the value product.  c: the scores' factor times log2(e).  kMask: keys behind a row's
+// limit, which only the last tiles have.
+// P is rounded to the type of the values: against f16 values (E4M3 codes, exact there) 2^-12
+// relative, against bf16 ones 2^-9, of the size of the output's own rounding.
+template <bool kF16Values, bool kMask>
+__device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int k0, float c,
+                                            const LaneOffsets<kF16Values>& at, const uint8_t* keys, uint32_t (&p)[16]) {
+  const int h = (threadIdx.x & 63) >> 5;
+  f32x16 s[2] = {(f32x16)(0.0f), (f32x16)(0.0f)};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(keys, 8 * (i & 1) + (i >> 1)), q[i >> 1], s[i & 1], 0, 0, 0);
+  sched<kSchedLdsRead, 4>();
+#pragma unroll
+  for (int i = 0; i < 12; ++i) {
+    sched<kSchedMfma, 1>();
+    sched<kSchedLdsRead, 1>();
+  }
+  sched<kSchedMfma, 4>();
+  if constexpr (kMask) {
+    const int from = row.limit - k0 - 4 * h;               // (key - k0 - 4 h above it: not visible)
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (k0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) > row.limit) s[b][i] = -INFINITY;
+        if (32 * b + 8 * (i >> 2) + (i & 3) > from) s[b][i] = -INFINITY;
   }
-  float mx = acc.m;
+  float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
-  mx = half_max(mx);
-  const float mc = fmaxf(mx * c, kNoScore);                // (finite where m is)
+  for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(s[0][i], s[1][i]), mx);
+  mx = fmaxf(acc.m, half_max(mx));
+  const float mc = fmaxf(mx * c, kNoScore);               // (finite where the maximum is)
   const float alpha = __builtin_amdgcn_exp2f(fmaf(acc.m, c, -mc));
   acc.m = mx;
   acc.l *= alpha;
@@ -164,9 +230,6 @@ __device__ __forceinline__ void attn_tile(AttnAcc& acc, const bf16x8 (&q)[8], co
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc.o[d][i] *= alpha;
-  // P rounded to the type of the values: against f16 values (E4M3 codes, exact there) 2^-12
-  // relative, against bf16 ones 2^-9, of the size of the output's own rounding.
-  uint32_t p[16];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -174,46 +237,58 @@ __device__ __forceinline__ void attn_tile(AttnAcc& acc, const bf16x8 (&q)[8], co
       const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -mc));
       const float e1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], c, -mc));
       acc.l += e0 + e1;
-      p[8 * b + i / 2] = kF16Values ? pack_f16(e0, e1) : pack_bf16(e0, e1);
+      p[8 * b + i / 2] = pack_p<kF16Values>(e0, e1);
     }
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const uint4 pw = make_uint4(p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]);
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      if constexpr (kF16Values) {
-        const f16x8 v = *reinterpret_cast<const f16x8*>(values + value16_at(t, h, 32 * d + j));
-        acc.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, __builtin_bit_cast(f16x8, pw), acc.o[d], 0, 0, 0);
-      } else {
-        // ds_read_b64_tr_b16: of 16 lanes that point at four rows x 16 columns, lane i gets column i
-        const int r = 16 * t + 4 * h + ((lane & 15) >> 2);
-        const int ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        const uint8_t* at = values + value_at(r, ch) + (lane & 1) * 8;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * 256));
-        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        acc.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pw), acc.o[d], 0, 0, 0);
-      }
-    }
-  }
 }
 
-// Keys and values of one tile from rows of bf16: token k0 + r at base + (k0 + r) * ld; rows from
-// `len` on are read as row len - 1 (no row attends to them: they only have to be finite).  1 KiB
-// (four rows) an instruction, straight into LDS, the chunks permuted by their source addresses.
-__device__ __forceinline__ void load_tile_bf16(const uint16_t* k, int64_t ld_k, const uint16_t* v, int64_t ld_v, int k0,
-                                               int len, uint8_t* keys, uint8_t* values) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// O^T += V^T P^T over the tile's values in LDS.
+template <bool kF16Values>
+__device__ __forceinline__ void attn_values(AttnAcc& acc, const uint32_t (&p)[16], const LaneOffsets<kF16Values>& at,
+                                            const uint8_t* values) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int o = wave * 4 + i;
-    const int r = 4 * o + (lane >> 4), ch = lane & 15;
-    const int64_t t = min(k0 + r, len - 1);
-    lds_dma16(reinterpret_cast<const uint8_t*>(k + t * ld_k + 8 * (ch ^ (r & 15))), keys + o * 1024);
-    lds_dma16(reinterpret_cast<const uint8_t*>(v + t * ld_v + 8 * (ch ^ ((r & 3) << 2))), values + o * 1024);
+  for (int i = 0; i < 16; ++i) {
+    const int t = i >> 2;
+    acc.o[i & 3] = value_mfma<kF16Values>(at.value(values, i), make_uint4(p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]), acc.o[i & 3]);
   }
+  constexpr int kReads = kF16Values ? 1 : 2;
+  sched<kSchedLdsRead, 3 * kReads>();
+#pragma unroll
+  for (int i = 0; i < 13; ++i) {
+    sched<kSchedMfma, 1>();
+    sched<kSchedLdsRead, kReads>();
+  }
+  sched<kSchedMfma, 3>();
 }
+
+// Rows of bf16 keys or values of one sequence (len rows of pitch ld), moved to LDS a tile at a time by
+// DMA, 1 KiB (four rows) an instruction, the chunks permuted by their source addresses.  The buffer
+// resource of a tile ends with the sequence's last row: rows behind it are not read and become 0.
+constexpr int kTileLoads = kTileBytes / 1024 / kAttnWaves;   // instructions a wave
+
+template <bool kValues>
+struct Bf16Rows {
+  const uint16_t* base;
+  int64_t ld;
+  int len;
+
+  __device__ __forceinline__ Bf16Rows(const uint16_t* b, int64_t pitch, int n) : base(b), ld(pitch), len(n) {}
+  __device__ __forceinline__ void load(int k0, uint8_t* tile) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+    const int first = k0 + 4 * kTileLoads * wave;            // this wave's rows
+    const int rows = min(len - first, 4 * kTileLoads);
+    const uint32_t bytes = rows > 0 ? (uint32_t)((rows - 1) * ld * 2) + 2 * kHeadDim : 0u;   // (ld < 2^24: below 2^29)
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + first * ld), (short)0, bytes, 0x00020000);
+    uint32_t lane;                                           // (made here, so that nothing is held across the loop)
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    const uint32_t four = lane >> 4, ch = 16 * ((lane & 15) ^ (kValues ? four << 2 : four));
+#pragma unroll
+    for (int i = 0; i < kTileLoads; ++i)
+      lds_dma16(r, (four + 4 * i) * (uint32_t)(2 * ld) + (kValues ? ch : ch ^ (64 * i)), 0,
+                tile + (wave * kTileLoads + i) * 1024);
+  }
+};
+static_assert(kTileLoads == 4, "a wave's rows start at a multiple of 16, so that chunk ^ 4 i permutes those of instruction i");
 
 // The same from pages of the FP8 cache: block ids table[k0 / 16 ..], pages past the last one
 // that holds a token below `len` repeat that one, ids outside the cache are clamped into it.
@@ -246,21 +321,42 @@ __device__ __forceinline__ int64_t page_offset(const PagedKv& c, int page) {
 
 // Thread t of 256: page (t >> 7) + 2 i of the tile for i = 0, 1; 16 bytes of keys, and of values
 // two dims x eight tokens (the two dwords of a half).
-struct Fp8TileRegs {
-  uint4 k[2];
-  uint2 va[2], vb[2];
-};
+struct Fp8Keys { uint4 w[2]; };
+struct Fp8Values { uint2 a[2], b[2]; };
+struct Fp8Pages { int64_t at[2]; };                       // this thread's pages' offsets in the cache
 
-__device__ __forceinline__ void fetch_tile_fp8(const PagedKv& c, int k0, int len, Fp8TileRegs& f) {
+__device__ __forceinline__ int tile_page(int i) { return (__builtin_amdgcn_readfirstlane(threadIdx.x) >> 7) + 2 * i; }
+
+__device__ __forceinline__ Fp8Pages tile_pages(const PagedKv& c, int k0, int len) {
+  Fp8Pages g;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) g.at[i] = page_offset(c, min(k0 / kPageTokens + tile_page(i), (len - 1) / kPageTokens));
+  return g;
+}
+
+__device__ __forceinline__ void fetch_keys(const PagedKv& c, const Fp8Pages& g, Fp8Keys& f) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) f.w[i] = *reinterpret_cast<const uint4*>(c.k + g.at[i] + (threadIdx.x & 127) * 16);
+}
+
+__device__ __forceinline__ void fetch_values(const PagedKv& c, const Fp8Pages& g, Fp8Values& f) {
   const int u = threadIdx.x & 127;
-  const int last = (len - 1) / kPageTokens;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int64_t base = page_offset(c, min(k0 / kPageTokens + (int)(threadIdx.x >> 7) + 2 * i, last));
-    f.k[i] = *reinterpret_cast<const uint4*>(c.k + base + u * 16);
-    const uint8_t* v = c.v + base + (u >> 6) * 512 + (u & 63) * 8;   // [a][dim][4], a = half, then half + 2
-    f.va[i] = *reinterpret_cast<const uint2*>(v);
-    f.vb[i] = *reinterpret_cast<const uint2*>(v + 1024);
+    const uint8_t* v = c.v + g.at[i] + (u >> 6) * 512 + (u & 63) * 8;     // [a][dim][4], a = half, then half + 2
+    f.a[i] = *reinterpret_cast<const uint2*>(v);
+    f.b[i] = *reinterpret_cast<const uint2*>(v + 1024);
+  }
+}
+
+__device__ __forceinline__ void store_keys(const Fp8Keys& f, uint8_t* keys) {
+  const int u = threadIdx.x & 127;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = tile_page(i) * kPageTokens + (u >> 3), ch = 2 * (u & 7);
+    const uint2 k0 = bf16_of_fp8(f.w[i].x), k1 = bf16_of_fp8(f.w[i].y), k2 = bf16_of_fp8(f.w[i].z), k3 = bf16_of_fp8(f.w[i].w);
+    *reinterpret_cast<uint4*>(keys + key_at(r, ch)) = make_uint4(k0.x, k0.y, k1.x, k1.y);
+    *reinterpret_cast<uint4*>(keys + key_at(r, ch + 1)) = make_uint4(k2.x, k2.y, k3.x, k3.y);
   }
 }
 
@@ -268,23 +364,99 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {   // the fir
   return n >= 4 ? w : (n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u));
 }
 
-__device__ __forceinline__ void store_tile_fp8(const Fp8TileRegs& f, int k0, int len, uint8_t* keys, uint8_t* values) {
-  const int u = threadIdx.x & 127;
+__device__ __forceinline__ void store_values(Fp8Values f, int k0, int len, uint8_t* values) {
+  const int u = threadIdx.x & 127, h = u >> 6, dim = 2 * (u & 63);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int page = (int)(threadIdx.x >> 7) + 2 * i;
-    const int r = page * kPageTokens + (u >> 3), ch = 2 * (u & 7);
-    const uint2 k0w = bf16_of_fp8(f.k[i].x), k1w = bf16_of_fp8(f.k[i].y), k2w = bf16_of_fp8(f.k[i].z),
-                k3w = bf16_of_fp8(f.k[i].w);
-    *reinterpret_cast<uint4*>(keys + key_at(r, ch)) = make_uint4(k0w.x, k0w.y, k1w.x, k1w.y);
-    *reinterpret_cast<uint4*>(keys + key_at(r, ch + 1)) = make_uint4(k2w.x, k2w.y, k3w.x, k3w.y);
-    const int h = u >> 6, dim = 2 * (u & 63);
-    const int na = len - (k0 + page * kPageTokens + 4 * h), nb = na - 8;   // tokens of the two dwords that exist
-    const uint2 a0 = f16_of_fp8(keep_bytes(f.va[i].x, na)), b0 = f16_of_fp8(keep_bytes(f.vb[i].x, nb));
-    const uint2 a1 = f16_of_fp8(keep_bytes(f.va[i].y, na)), b1 = f16_of_fp8(keep_bytes(f.vb[i].y, nb));
+    const int page = tile_page(i);
+    if (k0 + kTileKeys > len) {                            // (uniform) tokens of the two dwords that exist
+      const int na = len - (k0 + page * kPageTokens + 4 * h), nb = na - 8;
+      f.a[i] = make_uint2(keep_bytes(f.a[i].x, na), keep_bytes(f.a[i].y, na));
+      f.b[i] = make_uint2(keep_bytes(f.b[i].x, nb), keep_bytes(f.b[i].y, nb));
+    }
+    const uint2 a0 = f16_of_fp8(f.a[i].x), b0 = f16_of_fp8(f.b[i].x), a1 = f16_of_fp8(f.a[i].y), b1 = f16_of_fp8(f.b[i].y);
     *reinterpret_cast<uint4*>(values + value16_at(page, h, dim)) = make_uint4(a0.x, a0.y, b0.x, b0.y);
     *reinterpret_cast<uint4*>(values + value16_at(page, h, dim + 1)) = make_uint4(a1.x, a1.y, b1.x, b1.y);
   }
+}
+
+// All tiles of keys begin .. end - 1.  LDS holds one tile of keys and one of values, each refilled while
+// the other is in use: the values land under the score product, the next keys under the softmax and the
+// value product.  Two barriers a tile: behind the first (next_values) every wave has read the values
+// before and the keys are there, behind the second (next_keys) every wave has read the keys and the
+// values are there.  Keys and values are LDS objects of their own, so that the compiler sees that a
+// read of one need not wait for the other's loads.  32 KiB and at most 168 registers leave room for
+// three workgroups on a CU, whose matrix and vector work overlaps (32 heads over 4, 8191 and 16384
+// tokens: 2.63 ms, 1.04 PFLOP/s; two tiles of each in LDS, the score product of the next tile between
+// the instructions of this one's softmax, two workgroups: 2.75 ms, and short prompts took 1.7 times as
+// long; the library's largest bf16 product reaches 1.19 PFLOP/s here, at a clock that falls under load).
+// Tiles that every row sees in full come first and need no mask.
+struct TileLds {
+  uint8_t* k;
+  uint8_t* v;
+};
+
+template <bool kF16Values, class Keys, class Values>
+__device__ __forceinline__ void attn_run(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
+                                         float c, const TileLds& lds, Keys next_keys, Values next_values) {
+  c = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
+  const LaneOffsets<kF16Values> at;
+  uint32_t p[16];
+  int k0 = begin;
+  for (; k0 + kTileKeys - 1 <= row.all_limit; k0 += kTileKeys) {
+    next_values(k0);
+    attn_scores<kF16Values, false>(acc, q, row, k0, c, at, lds.k, p);
+    next_keys(k0 + kTileKeys);
+    attn_values<kF16Values>(acc, p, at, lds.v);
+  }
+  for (; k0 < end; k0 += kTileKeys) {
+    next_values(k0);
+    attn_scores<kF16Values, true>(acc, q, row, k0, c, at, lds.k, p);
+    next_keys(k0 + kTileKeys);
+    attn_values<kF16Values>(acc, p, at, lds.v);
+  }
+}
+
+__device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
+                                              float c, const Bf16Rows<false>& k, const Bf16Rows<true>& v,
+                                              const TileLds& lds) {
+  if (begin >= end) return;
+  k.load(begin, lds.k);
+  attn_run<false>(acc, q, row, begin, end, c, lds, [&](int k0) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    if (k0 < end) k.load(k0, lds.k);
+  }, [&](int k0) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    v.load(k0, lds.v);
+  });
+}
+
+// The same from the FP8 cache, through registers, where the codes are widened: codes are loaded a
+// step before they are stored, page ids another before that.
+__device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
+                                             float c, const PagedKv& pages, int len, const TileLds& lds) {
+  if (begin >= end) return;
+  Fp8Keys fk;
+  Fp8Values fv;
+  Fp8Pages at = tile_pages(pages, begin, len);
+  fetch_keys(pages, at, fk);
+  fetch_values(pages, at, fv);
+  at = tile_pages(pages, begin + kTileKeys, len);
+  store_keys(fk, lds.k);
+  fetch_keys(pages, at, fk);
+  attn_run<true>(acc, q, row, begin, end, c, lds, [&](int k0) {
+    lds_barrier();
+    if (k0 >= end) return;
+    store_keys(fk, lds.k);
+    at = tile_pages(pages, k0 + kTileKeys, len);
+    fetch_keys(pages, at, fk);
+  }, [&](int k0) {
+    lds_barrier();
+    store_values(fv, k0, len, lds.v);
+    fetch_values(pages, at, fv);
+  });
 }
 
 // Dims 32 d + 8 g + 4 h .. + 3 of this lane's row, of the eight that the half's pair of lanes share:

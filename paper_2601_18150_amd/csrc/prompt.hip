@@ -43,12 +43,15 @@ struct PromptArgs {
 
 template <bool kFp8>
 __global__ __launch_bounds__(kMfmaBounds) void attn_prompt_kernel(const PromptArgs p) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTileBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kTileBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_values[kTileBytes];
+  const TileLds lds{lds_keys, lds_values};
   const int kvh = blockIdx.x % p.kv_heads, tiles = gridDim.x / p.kv_heads;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TileOf at;
   if (!find_tile(p.cu_seqlens, p.batch, p.total, p.group_log2, tiles - 1 - (int)(blockIdx.x / p.kv_heads), at)) return;
+  at.to_scalars();
   const int group = 1 << p.group_log2;
   const int len = kFp8 ? min(max(p.seq_lens[at.b], 0), p.max_seq_len) : at.n;
   const int first = len - at.n;                         // position of the call's first token of the sequence
@@ -60,7 +63,6 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_prompt_kernel(const PromptAr
   AttnRow row;
   row.q = p.q + token * p.ld_q + head * kHeadDim;
   row.limit = position(r);
-  row.wave_limit = position(row0 + kRowsPerWave * wave);
   row.wave_last = position(row0 + kRowsPerWave * wave + kRowsPerWave - 1);
   const int split = blockIdx.y;
   const int begin = split * p.split_keys;
@@ -68,6 +70,7 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_prompt_kernel(const PromptAr
   if (p.splits > 1 && split == 0 && kvh == 0 && (r & (group - 1)) == 0 && r < rows && lane < 32)
     p.counts[token] = row.limit < 0 ? 0 : row.limit / p.split_keys + 1;
   if (begin >= end && p.splits > 1) return;
+  row.all_limit = min(position(row0), end - 1);
 
   AttnAcc acc;
   attn_init(acc);
@@ -75,23 +78,14 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_prompt_kernel(const PromptAr
   attn_load_q(row, q);
   const float sscale = (kFp8 ? p.k_scale[0] : 1.0f) * p.sm_scale;
   const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
-  uint8_t* keys = lds;
-  uint8_t* values = lds + kTileBytes;
-  for (int k0 = begin; k0 < end; k0 += kTileKeys) {
-    lds_barrier();                                      // every wave has read the tile before
-    if constexpr (kFp8) {
-      const PagedKv c8{static_cast<const uint8_t*>(p.k), static_cast<const uint8_t*>(p.v),
-                       p.block_table + (int64_t)at.b * p.max_blocks, p.num_blocks, p.max_blocks, p.kv_heads, kvh};
-      Fp8TileRegs f;
-      fetch_tile_fp8(c8, k0, len, f);
-      store_tile_fp8(f, k0, len, keys, values);
-    } else {
-      load_tile_bf16(static_cast<const uint16_t*>(p.k) + at.first * p.ld_k + kvh * kHeadDim, p.ld_k,
-                     static_cast<const uint16_t*>(p.v) + at.first * p.ld_v + kvh * kHeadDim, p.ld_v, k0, len, keys, values);
-      wait_vmcnt<0>();
-    }
-    lds_barrier();
-    if (k0 <= row.wave_last) attn_tile<kFp8>(acc, q, row, k0, c, keys, values);
+  if constexpr (kFp8) {
+    const PagedKv pages{static_cast<const uint8_t*>(p.k), static_cast<const uint8_t*>(p.v),
+                        p.block_table + (int64_t)at.b * p.max_blocks, p.num_blocks, p.max_blocks, p.kv_heads, kvh};
+    attn_run_fp8(acc, q, row, begin, end, c, pages, len, lds);
+  } else {
+    const Bf16Rows<false> k(static_cast<const uint16_t*>(p.k) + at.first * p.ld_k + kvh * kHeadDim, p.ld_k, len);
+    const Bf16Rows<true> v(static_cast<const uint16_t*>(p.v) + at.first * p.ld_v + kvh * kHeadDim, p.ld_v, len);
+    attn_run_bf16(acc, q, row, begin, end, c, k, v, lds);
   }
   const float l = half_sum(acc.l);
   const bool valid = r < rows;

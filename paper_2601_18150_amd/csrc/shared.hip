@@ -47,7 +47,10 @@ __device__ __forceinline__ int wave_min(int v) {
 
 // Rows: member r / G of the group, query head r % G of the kv head's.
 __global__ __launch_bounds__(kMfmaBounds) void attn_shared_prefix_kernel(const SharedArgs p) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTileBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kTileBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_values[kTileBytes];
+  __shared__ int smallest[kAttnWaves];
+  const TileLds lds{lds_keys, lds_values};
   const int kvh = blockIdx.x % p.kv_heads, split = blockIdx.y;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -58,6 +61,7 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_shared_prefix_kernel(const S
   }
   TileOf at;
   if (!find_tile(p.group_offsets, p.groups, p.batch, p.group_log2, blockIdx.x / p.kv_heads, at)) return;
+  at.to_scalars();
   const int group = 1 << p.group_log2;
   const int rows = at.n << p.group_log2, row0 = at.index * kAttnRows;
   // the part that is shared: whole pages of the first member's
@@ -71,8 +75,11 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_shared_prefix_kernel(const S
   AttnRow row;
   row.q = p.q + ((int64_t)seq * p.kv_heads * group + head) * kHeadDim;
   row.limit = min(clamped_len(p, seq), prefix) - 1;     // (a member may be shorter than the prefix)
-  row.wave_limit = wave_min(row.limit);
   row.wave_last = -wave_min(-row.limit);
+  const int least = wave_min(row.limit);
+  if (lane == 0) smallest[wave] = least;
+  __syncthreads();
+  row.all_limit = min(min(min(smallest[0], smallest[1]), min(smallest[2], smallest[3])), end - 1);
 
   AttnAcc acc;
   attn_init(acc);
@@ -80,17 +87,8 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_shared_prefix_kernel(const S
   attn_load_q(row, q);
   const float sscale = p.k_scale[0] * p.sm_scale;
   const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
-  uint8_t* keys = lds;
-  uint8_t* values = lds + kTileBytes;
   const PagedKv pages{p.k, p.v, p.block_table + (int64_t)at.first * p.max_blocks, p.num_blocks, p.max_blocks, p.kv_heads, kvh};
-  for (int k0 = begin; k0 < end; k0 += kTileKeys) {
-    Fp8TileRegs f;
-    fetch_tile_fp8(pages, k0, prefix, f);
-    lds_barrier();                                      // every wave has read the tile before
-    store_tile_fp8(f, k0, prefix, keys, values);
-    lds_barrier();
-    if (k0 <= row.wave_last) attn_tile<true>(acc, q, row, k0, c, keys, values);
-  }
+  attn_run_fp8(acc, q, row, begin, end, c, pages, prefix, lds);
   const float l = half_sum(acc.l);
   const bool valid = r < rows;
   const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;

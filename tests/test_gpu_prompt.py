@@ -78,6 +78,18 @@ def test_prompt_from_a_fused_output_into_a_padded_one(fp8rl):
     assert torch.all(rows[:4] == 7.0) and torch.all(rows[131:] == 7.0) and torch.all(out[:, heads * 128:] == 7.0)
 
 
+def test_prompt_sees_nothing_of_the_call_before(fp8rl):
+    """Rows behind a short sequence's end, inside its tiles, count as zeros whatever LDS held before (here NaN)."""
+    announce("prompt: short sequences after a call with NaN everywhere")
+    rng = np.random.default_rng(16)
+    nan = torch.full((20000, 8, 128), float("nan"), dtype=torch.bfloat16)
+    run_prompt(fp8rl, nan, nan, nan, [0, 20000])
+    lengths = rng.integers(1, 40, 500)
+    cu, n = offsets(lengths), int(lengths.sum())
+    q, k, v = (bf16(rng, (n, 1, 128)) for _ in range(3))
+    check(run_prompt(fp8rl, q, k, v, cu), attention.prompt(u16(q), u16(k), u16(v), cu, SM), 40, attention.BF16_VALUES, "prompt")
+
+
 @pytest.mark.parametrize("sm", [1e-38, 3.0, 40.0])
 def test_prompt_extreme_factors(fp8rl, sm):
     """A factor that makes every weight 1, and ones that make each row all but one key's."""
