@@ -190,6 +190,52 @@ __device__ __forceinline__ uint32_t pack_p(float a, float b) {
   return kF16Values ? pack_f16(a, b) : pack_bf16(a, b);
 }
 
+// A row's maximum is only followed once it has grown by this much (a factor of 2^8 in P), so that its
+// accumulator is rarely scaled.  P stays at most 2^8 (fp16 holds 2^16), and every sum at least 1.
+constexpr float kMaxGrowth = 8.0f;
+
+// o *= alpha, where any row needs it (any: a bit per lane).  The branches are inside the assembly: as a
+// branch of the program the compiler keeps the accumulators in two places and copies all of them past
+// it in every tile (32 heads over 4, 8191 and 16384 tokens: 2.80 ms; always scaled 2.63; so 2.54).  The products
+// that made o have ended: alpha comes out of products issued after them.
+__device__ __forceinline__ void scale_if(uint64_t any, f32x16 (&o)[4], float alpha) {
+  asm volatile("s_cmp_eq_u64 %14, 0\n\ts_cbranch_scc1 L%=_as_it_is\n\tv_mul_f32 %0, %0, %13\n\tv_mul_f32 %1, %1, %13\n\t"
+      "v_mul_f32 %2, %2, %13\n\tv_mul_f32 %3, %3, %13\n\tv_mul_f32 %4, %4, %13\n\tv_mul_f32 %5, %5, %13\n\t"
+      "v_mul_f32 %6, %6, %13\n\tv_mul_f32 %7, %7, %13\n\tv_mul_f32 %8, %8, %13\n\tv_mul_f32 %9, %9, %13\n\t"
+      "v_mul_f32 %10, %10, %13\n\tv_mul_f32 %11, %11, %13\n\tv_mul_f32 %12, %12, %13\n\tL%=_as_it_is:"
+      : "+v"(o[0][0]), "+v"(o[0][1]), "+v"(o[0][2]), "+v"(o[0][3]), "+v"(o[0][4]), "+v"(o[0][5]), "+v"(o[0][6]),
+      "+v"(o[0][7]), "+v"(o[0][8]), "+v"(o[0][9]), "+v"(o[0][10]), "+v"(o[0][11]), "+v"(o[0][12])
+      : "v"(alpha), "s"(any) : "scc");
+  asm volatile("s_cmp_eq_u64 %14, 0\n\ts_cbranch_scc1 L%=_as_it_is\n\tv_mul_f32 %0, %0, %13\n\tv_mul_f32 %1, %1, %13\n\t"
+      "v_mul_f32 %2, %2, %13\n\tv_mul_f32 %3, %3, %13\n\tv_mul_f32 %4, %4, %13\n\tv_mul_f32 %5, %5, %13\n\t"
+      "v_mul_f32 %6, %6, %13\n\tv_mul_f32 %7, %7, %13\n\tv_mul_f32 %8, %8, %13\n\tv_mul_f32 %9, %9, %13\n\t"
+      "v_mul_f32 %10, %10, %13\n\tv_mul_f32 %11, %11, %13\n\tv_mul_f32 %12, %12, %13\n\tL%=_as_it_is:"
+      : "+v"(o[0][13]), "+v"(o[0][14]), "+v"(o[0][15]), "+v"(o[1][0]), "+v"(o[1][1]), "+v"(o[1][2]), "+v"(o[1][3]),
+      "+v"(o[1][4]), "+v"(o[1][5]), "+v"(o[1][6]), "+v"(o[1][7]), "+v"(o[1][8]), "+v"(o[1][9])
+      : "v"(alpha), "s"(any) : "scc");
+  asm volatile("s_cmp_eq_u64 %14, 0\n\ts_cbranch_scc1 L%=_as_it_is\n\tv_mul_f32 %0, %0, %13\n\tv_mul_f32 %1, %1, %13\n\t"
+      "v_mul_f32 %2, %2, %13\n\tv_mul_f32 %3, %3, %13\n\tv_mul_f32 %4, %4, %13\n\tv_mul_f32 %5, %5, %13\n\t"
+      "v_mul_f32 %6, %6, %13\n\tv_mul_f32 %7, %7, %13\n\tv_mul_f32 %8, %8, %13\n\tv_mul_f32 %9, %9, %13\n\t"
+      "v_mul_f32 %10, %10, %13\n\tv_mul_f32 %11, %11, %13\n\tv_mul_f32 %12, %12, %13\n\tL%=_as_it_is:"
+      : "+v"(o[1][10]), "+v"(o[1][11]), "+v"(o[1][12]), "+v"(o[1][13]), "+v"(o[1][14]), "+v"(o[1][15]),
+      "+v"(o[2][0]), "+v"(o[2][1]), "+v"(o[2][2]), "+v"(o[2][3]), "+v"(o[2][4]), "+v"(o[2][5]), "+v"(o[2][6])
+      : "v"(alpha), "s"(any) : "scc");
+  asm volatile("s_cmp_eq_u64 %14, 0\n\ts_cbranch_scc1 L%=_as_it_is\n\tv_mul_f32 %0, %0, %13\n\tv_mul_f32 %1, %1, %13\n\t"
+      "v_mul_f32 %2, %2, %13\n\tv_mul_f32 %3, %3, %13\n\tv_mul_f32 %4, %4, %13\n\tv_mul_f32 %5, %5, %13\n\t"
+      "v_mul_f32 %6, %6, %13\n\tv_mul_f32 %7, %7, %13\n\tv_mul_f32 %8, %8, %13\n\tv_mul_f32 %9, %9, %13\n\t"
+      "v_mul_f32 %10, %10, %13\n\tv_mul_f32 %11, %11, %13\n\tv_mul_f32 %12, %12, %13\n\tL%=_as_it_is:"
+      : "+v"(o[2][7]), "+v"(o[2][8]), "+v"(o[2][9]), "+v"(o[2][10]), "+v"(o[2][11]), "+v"(o[2][12]), "+v"(o[2][13]),
+      "+v"(o[2][14]), "+v"(o[2][15]), "+v"(o[3][0]), "+v"(o[3][1]), "+v"(o[3][2]), "+v"(o[3][3])
+      : "v"(alpha), "s"(any) : "scc");
+  asm volatile("s_cmp_eq_u64 %13, 0\n\ts_cbranch_scc1 L%=_as_it_is\n\tv_mul_f32 %0, %0, %12\n\tv_mul_f32 %1, %1, %12\n\t"
+      "v_mul_f32 %2, %2, %12\n\tv_mul_f32 %3, %3, %12\n\tv_mul_f32 %4, %4, %12\n\tv_mul_f32 %5, %5, %12\n\t"
+      "v_mul_f32 %6, %6, %12\n\tv_mul_f32 %7, %7, %12\n\tv_mul_f32 %8, %8, %12\n\tv_mul_f32 %9, %9, %12\n\t"
+      "v_mul_f32 %10, %10, %12\n\tv_mul_f32 %11, %11, %12\n\tL%=_as_it_is:"
+      : "+v"(o[3][4]), "+v"(o[3][5]), "+v"(o[3][6]), "+v"(o[3][7]), "+v"(o[3][8]), "+v"(o[3][9]), "+v"(o[3][10]),
+      "+v"(o[3][11]), "+v"(o[3][12]), "+v"(o[3][13]), "+v"(o[3][14]), "+v"(o[3][15])
+      : "v"(alpha), "s"(any) : "scc");
+}
+
 // Scores of the tile of keys k0 .. k0 + 63 in LDS, and P from them (in the type of the values), in
 // the order of the value product.  c: the scores' factor times log2(e).  kMask: keys behind a row's
 // limit, which only the last tiles have.
@@ -221,15 +267,14 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
   float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
   for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(s[0][i], s[1][i]), mx);
-  mx = fmaxf(acc.m, half_max(mx));
-  const float mc = fmaxf(mx * c, kNoScore);               // (finite where the maximum is)
+  mx = half_max(mx);
+  const bool grown = (mx - acc.m) * c > kMaxGrowth;       // (of this row alone: rows do not affect each other)
+  const float m = grown ? mx : acc.m;
+  const float mc = fmaxf(m * c, kNoScore);                // (finite where the maximum is)
   const float alpha = __builtin_amdgcn_exp2f(fmaf(acc.m, c, -mc));
-  acc.m = mx;
+  acc.m = m;
   acc.l *= alpha;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc.o[d][i] *= alpha;
+  scale_if(__ballot(grown), acc.o, alpha);
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -313,39 +358,46 @@ struct PagedKv {
   int max_blocks, kv_heads, kvh;
 };
 
-__device__ __forceinline__ int64_t page_offset(const PagedKv& c, int page) {
-  const int blk = c.table[min(page, c.max_blocks - 1)];
+// (the table does not change under the kernel: a scalar load)
+__device__ __forceinline__ int page_entry(const PagedKv& c, int page) {
+  typedef const __attribute__((address_space(4))) int32_t const_i32;
+  return *(const_i32*)(c.table + min(page, c.max_blocks - 1));
+}
+
+__device__ __forceinline__ int64_t page_offset(const PagedKv& c, int blk) {
   const int64_t b = blk < 0 ? 0 : ((int64_t)blk >= c.num_blocks ? c.num_blocks - 1 : blk);
   return (b * c.kv_heads + c.kvh) * (kPageTokens * kHeadDim);
 }
 
-// Thread t of 256: page (t >> 7) + 2 i of the tile for i = 0, 1; 16 bytes of keys, and of values
-// two dims x eight tokens (the two dwords of a half).
+// Thread t of 256: pages t / 128 and t / 128 + 2 of the tile; 16 bytes of keys each, and of values the
+// dwords of dims L and L + 64 of tokens 4 h .. and 4 h + 8 .., with L = t % 64 and h = t / 64 % 2.
 struct Fp8Keys { uint4 w[2]; };
-struct Fp8Values { uint2 a[2], b[2]; };
-struct Fp8Pages { int64_t at[2]; };                       // this thread's pages' offsets in the cache
+struct Fp8Values { uint32_t w[2][4]; };                   // dim L of both fours, dim L + 64 of both
+struct Fp8Pages { int blk[2]; };                          // this wave's pages' entries in the block table
 
-__device__ __forceinline__ int tile_page(int i) { return (__builtin_amdgcn_readfirstlane(threadIdx.x) >> 7) + 2 * i; }
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6; }
+__device__ __forceinline__ int tile_page(int i) { return (wave_of() >> 1) + 2 * i; }
 
 __device__ __forceinline__ Fp8Pages tile_pages(const PagedKv& c, int k0, int len) {
   Fp8Pages g;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) g.at[i] = page_offset(c, min(k0 / kPageTokens + tile_page(i), (len - 1) / kPageTokens));
+  for (int i = 0; i < 2; ++i) g.blk[i] = page_entry(c, min(k0 / kPageTokens + tile_page(i), (len - 1) / kPageTokens));
   return g;
 }
 
 __device__ __forceinline__ void fetch_keys(const PagedKv& c, const Fp8Pages& g, Fp8Keys& f) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) f.w[i] = *reinterpret_cast<const uint4*>(c.k + g.at[i] + (threadIdx.x & 127) * 16);
+  for (int i = 0; i < 2; ++i)
+    f.w[i] = *reinterpret_cast<const uint4*>(c.k + page_offset(c, g.blk[i]) + (threadIdx.x & 127) * 16);
 }
 
 __device__ __forceinline__ void fetch_values(const PagedKv& c, const Fp8Pages& g, Fp8Values& f) {
-  const int u = threadIdx.x & 127;
+  const int lane = threadIdx.x & 63, h = wave_of() & 1;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint8_t* v = c.v + g.at[i] + (u >> 6) * 512 + (u & 63) * 8;     // [a][dim][4], a = half, then half + 2
-    f.a[i] = *reinterpret_cast<const uint2*>(v);
-    f.b[i] = *reinterpret_cast<const uint2*>(v + 1024);
+    const uint32_t* v = reinterpret_cast<const uint32_t*>(c.v + page_offset(c, g.blk[i])) + h * kHeadDim + lane;   // [a][dim]
+#pragma unroll
+    for (int u = 0; u < 4; ++u) f.w[i][u] = v[(u & 1) * 2 * kHeadDim + (u >> 1) * 64];
   }
 }
 
@@ -365,18 +417,19 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {   // the fir
 }
 
 __device__ __forceinline__ void store_values(Fp8Values f, int k0, int len, uint8_t* values) {
-  const int u = threadIdx.x & 127, h = u >> 6, dim = 2 * (u & 63);
+  const int lane = threadIdx.x & 63, h = wave_of() & 1;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int page = tile_page(i);
-    if (k0 + kTileKeys > len) {                            // (uniform) tokens of the two dwords that exist
-      const int na = len - (k0 + page * kPageTokens + 4 * h), nb = na - 8;
-      f.a[i] = make_uint2(keep_bytes(f.a[i].x, na), keep_bytes(f.a[i].y, na));
-      f.b[i] = make_uint2(keep_bytes(f.b[i].x, nb), keep_bytes(f.b[i].y, nb));
+    if (k0 + kTileKeys > len) {                            // (uniform) tokens of the fours that exist
+      const int n = len - (k0 + tile_page(i) * kPageTokens + 4 * h);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) f.w[i][u] = keep_bytes(f.w[i][u], n - 8 * (u & 1));
     }
-    const uint2 a0 = f16_of_fp8(f.a[i].x), b0 = f16_of_fp8(f.b[i].x), a1 = f16_of_fp8(f.a[i].y), b1 = f16_of_fp8(f.b[i].y);
-    *reinterpret_cast<uint4*>(values + value16_at(page, h, dim)) = make_uint4(a0.x, a0.y, b0.x, b0.y);
-    *reinterpret_cast<uint4*>(values + value16_at(page, h, dim + 1)) = make_uint4(a1.x, a1.y, b1.x, b1.y);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint2 a = f16_of_fp8(f.w[i][2 * u]), b = f16_of_fp8(f.w[i][2 * u + 1]);
+      *reinterpret_cast<uint4*>(values + value16_at(tile_page(i), h, lane + 64 * u)) = make_uint4(a.x, a.y, b.x, b.y);
+    }
   }
 }
 
@@ -433,27 +486,30 @@ __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8]
   });
 }
 
-// The same from the FP8 cache, through registers, where the codes are widened: codes are loaded a
-// step before they are stored, page ids another before that.
+// The same from the FP8 cache, through registers, where the codes are widened: a tile's codes are asked
+// for when those of the one before it have been stored, its page ids a step earlier.  What is asked for
+// behind the last tile repeats the last pages.  (The codes held in registers leave room for two
+// workgroups on a CU; brought through LDS by DMA instead, three of them took as long over long
+// contexts and a tenth longer over short ones.)
 __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
                                              float c, const PagedKv& pages, int len, const TileLds& lds) {
   if (begin >= end) return;
   Fp8Keys fk;
   Fp8Values fv;
-  Fp8Pages at = tile_pages(pages, begin, len);
+  Fp8Pages at = tile_pages(pages, begin, len), after = tile_pages(pages, begin + kTileKeys, len);
   fetch_keys(pages, at, fk);
   fetch_values(pages, at, fv);
-  at = tile_pages(pages, begin + kTileKeys, len);
+  at = after;                                              // of the tile whose values are asked for next
   store_keys(fk, lds.k);
   fetch_keys(pages, at, fk);
   attn_run<true>(acc, q, row, begin, end, c, lds, [&](int k0) {
     lds_barrier();
-    if (k0 >= end) return;
     store_keys(fk, lds.k);
-    at = tile_pages(pages, k0 + kTileKeys, len);
-    fetch_keys(pages, at, fk);
+    fetch_keys(pages, after, fk);
+    at = after;
   }, [&](int k0) {
     lds_barrier();
+    after = tile_pages(pages, k0 + 2 * kTileKeys, len);
     store_values(fv, k0, len, lds.v);
     fetch_values(pages, at, fv);
   });

@@ -42,7 +42,7 @@ struct PromptArgs {
 };
 
 template <bool kFp8>
-__global__ __launch_bounds__(kMfmaBounds) void attn_prompt_kernel(const PromptArgs p) {
+__global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_kernel(const PromptArgs p) {
   __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t lds_values[kTileBytes];
   const TileLds lds{lds_keys, lds_values};

@@ -46,7 +46,7 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 
 // Rows: member r / G of the group, query head r % G of the kv head's.
-__global__ __launch_bounds__(kMfmaBounds) void attn_shared_prefix_kernel(const SharedArgs p) {
+__global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_shared_prefix_kernel(const SharedArgs p) {
   __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t lds_values[kTileBytes];
   __shared__ int smallest[kAttnWaves];
