@@ -459,7 +459,7 @@ int fp8rl_attention_decode_bf16kv(const uint16_t* q, const uint16_t* k_cache, co
  *      total (precondition; offsets are clamped into [0, total], so that nothing outside the rows is
  *      touched).  Sequences may be empty; rows before the first offset or from the last one on are
  *      read by no sequence and written by none.
- * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; total * q_heads / 128 + batch * kv_heads < 2^23
+ * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; total * q_heads / 128 + 2 * batch * kv_heads < 2^23
  * (else FP8RL_ERR_UNSUPPORTED_SHAPE).  total == 0 or batch == 0 is a no-op.
  * Alignment: q, k, v, out 16-byte, every ld a multiple of 8, cu_seqlens 4-byte.
  */
@@ -513,7 +513,7 @@ int fp8rl_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const uint8_t*
  * workspace      fp8rl_attention_decode_shared_workspace_size(batch, num_groups, q_heads, kv_heads,
  *                max_prefix_len, max_seq_len) bytes, 16-byte aligned, not shared by calls (or captured
  *                graphs) that may overlap
- * num_groups 1 .. 65535; everything else as for fp8rl_attention_decode_fp8kv.
+ * num_groups 1 .. 65535, batch * q_heads < 2^22; everything else as for fp8rl_attention_decode_fp8kv.
  */
 int64_t fp8rl_attention_decode_shared_workspace_size(int64_t batch, int64_t num_groups, int64_t q_heads,
                                                      int64_t kv_heads, int64_t max_prefix_len, int64_t max_seq_len);

@@ -9,6 +9,8 @@
 
 namespace {
 
+constexpr int64_t kMaxGrid = int64_t(1) << 23;   // workgroups (of 256 threads: HIP takes 2^32 threads less one)
+
 // Heads and factor that every attention entry point takes: an FP8RL_* error, or kLaunch.
 int check_heads(int64_t q_heads, int64_t kv_heads, int64_t head_dim, float sm_scale) {
   if (kv_heads < 1 || q_heads < 1) return FP8RL_ERR_INVALID_ARG;
@@ -22,13 +24,14 @@ int check_heads(int64_t q_heads, int64_t kv_heads, int64_t head_dim, float sm_sc
 // Packed rows: sizes, then the rows of q and out.
 int check_prompt(const uint16_t* q, int64_t ld_q, const int32_t* cu_seqlens, int64_t batch, int64_t total,
                  int64_t q_heads, int64_t kv_heads, int64_t head_dim, float sm_scale, const uint16_t* out,
-                 int64_t ld_out) {
+                 int64_t ld_out, bool fp8) {
   if (batch < 0 || total < 0) return FP8RL_ERR_INVALID_ARG;
   const int st = check_heads(q_heads, kv_heads, head_dim, sm_scale);
   if (st != kLaunch) return st;
-  if (batch >= kMaxDim || total >= kMaxDim || total * q_heads / 128 + batch * kv_heads >= (int64_t(1) << 23))
-    return FP8RL_ERR_UNSUPPORTED_SHAPE;
+  if (batch >= kMaxDim || total >= kMaxDim) return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (batch == 0 || total == 0) return FP8RL_OK;
+  if (fp8rl::attn_prompt_workgroups(batch, total, q_heads / kv_heads, kv_heads, fp8) >= kMaxGrid)
+    return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (!q || !cu_seqlens || !out) return FP8RL_ERR_INVALID_ARG;
   if (ld_q < q_heads * 128 || ld_out < q_heads * 128) return FP8RL_ERR_INVALID_ARG;
   if (ld_q >= kMaxDim || ld_out >= kMaxDim) return FP8RL_ERR_UNSUPPORTED_SHAPE;
@@ -84,7 +87,7 @@ int fp8rl_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t*
                                 int64_t kv_heads, int64_t head_dim, float sm_scale, uint16_t* out, int64_t ld_out,
                                 void* stream) {
   const int st =
-      check_prompt(q, ld_q, cu_seqlens, batch, total, q_heads, kv_heads, head_dim, sm_scale, out, ld_out);
+      check_prompt(q, ld_q, cu_seqlens, batch, total, q_heads, kv_heads, head_dim, sm_scale, out, ld_out, false);
   if (st != kLaunch) return st;
   if (!k || !v) return FP8RL_ERR_INVALID_ARG;
   if (ld_k < kv_heads * 128 || ld_v < kv_heads * 128) return FP8RL_ERR_INVALID_ARG;
@@ -112,7 +115,7 @@ int fp8rl_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const uint8_t*
   if (max_seq_len < 0 || num_blocks < 0 || max_blocks < 0 || workspace_bytes < 0) return FP8RL_ERR_INVALID_ARG;
   if (max_seq_len >= (int64_t(1) << 30) || max_blocks >= kMaxDim || num_blocks >= kMaxDim)
     return FP8RL_ERR_UNSUPPORTED_SHAPE;
-  int st = check_prompt(q, ld_q, cu_seqlens, batch, total, q_heads, kv_heads, head_dim, sm_scale, out, ld_out);
+  int st = check_prompt(q, ld_q, cu_seqlens, batch, total, q_heads, kv_heads, head_dim, sm_scale, out, ld_out, true);
   if (st != kLaunch) return st;
   st = check_paged(k_cache, v_cache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale, v_scale);
   if (st != kLaunch) return st;
@@ -150,8 +153,11 @@ int fp8rl_attention_decode_shared_fp8kv(const uint16_t* q, const uint8_t* k_cach
   if (batch > 65535 || num_groups > 65535 || max_seq_len >= (int64_t(1) << 30) || max_blocks >= kMaxDim ||
       num_blocks >= kMaxDim)
     return FP8RL_ERR_UNSUPPORTED_SHAPE;
-  if (batch * q_heads / 128 + num_groups * kv_heads >= (int64_t(1) << 23)) return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (batch == 0) return FP8RL_OK;
+  if (batch * q_heads >= kMaxGrid ||
+      fp8rl::attn_shared_workgroups(batch, num_groups, q_heads / kv_heads, kv_heads, max_prefix_len, max_seq_len) >=
+          kMaxGrid)
+    return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (!q || !out || !group_offsets || !prefix_lens || !workspace) return FP8RL_ERR_INVALID_ARG;
   st = check_paged(k_cache, v_cache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale, v_scale);
   if (st != kLaunch) return st;

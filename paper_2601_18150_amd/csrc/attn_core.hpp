@@ -51,7 +51,10 @@ __device__ __forceinline__ int value_at(int r, int c) { return r * 256 + ((c ^ (
 // (16-key step, half, dim), the eight keys of that half in the order of the value product.
 __device__ __forceinline__ int value16_at(int step, int h, int dim) { return ((step * 2 + h) * kHeadDim + dim) * 16; }
 
-// Sequence of tile `t`, each with ceil(length * G / 128) of them, and the tile's index inside it.
+// Rows of a tile of a run of `rows`: 128, or 32 where `small` says that so few rows take those.
+__device__ __forceinline__ int tile_rows(int64_t rows, int small) { return rows <= small ? kRowsPerWave : kAttnRows; }
+
+// Sequence of tile `t`, each with ceil(length * G / rows of a tile) of them, and the tile's index inside it.
 // Offsets are clamped into [0, total], lengths below 0 count as 0.  false: behind the last tile.
 struct TileOf {
   int b, index, first, n;      // sequence, tile inside it, its first token, its tokens
@@ -64,14 +67,15 @@ struct TileOf {
   }
 };
 
-__device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int total, int group_log2, int t, TileOf& out) {
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int total, int group_log2, int small, int t, TileOf& out) {
   const int lane = threadIdx.x & 63;
   int before = 0;
   for (int base = 0; base < count; base += 64) {
     const int i = base + lane;
     const int lo = min(max(offsets[min(i, count)], 0), total), hi = min(max(offsets[min(i + 1, count)], 0), total);
     const int n = i < count ? max(hi - lo, 0) : 0;
-    const int tiles = (int)((((int64_t)n << group_log2) + kAttnRows - 1) / kAttnRows);
+    const int64_t rows = (int64_t)n << group_log2;
+    const int tiles = (int)((rows + tile_rows(rows, small) - 1) / tile_rows(rows, small));
     const int sum = wave_inclusive_sum(tiles);
     const uint64_t hit = __ballot(before + sum > t);
     if (hit) {
@@ -87,8 +91,20 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int
   return false;
 }
 
-// Tiles of all runs: an upper bound, each run's last one may be partly filled.
-inline int64_t attn_tile_bound(int64_t rows, int64_t runs) { return rows / kAttnRows + runs; }
+// Tiles of all runs: an upper bound (each run's last one may be partly filled).
+inline int64_t attn_tile_bound(int64_t rows, int64_t runs, int small) {
+  if (small == 0) return rows / kAttnRows + runs;
+  const int64_t mixed = rows / kAttnRows + runs * ((small + kRowsPerWave - 1) / kRowsPerWave);
+  const int64_t all_small = rows / kRowsPerWave + runs;
+  return mixed < all_small ? mixed : all_small;
+}
+
+// The tiles if the runs were all as long as their mean (what a rule that fills the chip goes by).
+inline int64_t attn_tile_guess(int64_t rows, int64_t runs, int small) {
+  const int64_t mean = (rows + runs - 1) / (runs > 0 ? runs : 1);
+  const int64_t tile = mean <= small ? kRowsPerWave : kAttnRows;
+  return runs * ((mean + tile - 1) / tile);
+}
 
 inline int group_log2_of(int64_t g) { return g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3; }
 
@@ -348,6 +364,12 @@ __device__ __forceinline__ uint2 bf16_of_fp8(uint32_t w) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, false);
   const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, true);
   return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+
+// This wave's LDS reads have ended.
+__device__ __forceinline__ void wait_lds() {
+  __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));
+  asm volatile("" ::: "memory");
 }
 
 struct PagedKv {

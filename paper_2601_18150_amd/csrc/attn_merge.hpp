@@ -24,14 +24,6 @@ constexpr int rec_m() { return kG * 128; }
 template <int kG>
 constexpr int rec_l() { return kG * 128 + kG; }
 
-constexpr int kRestMinPages = 16;
-
-// Pages per record of a sequence's part from page `from` on, divided over `records`.
-__device__ __forceinline__ int rest_split_pages(int len, int from, int records) {
-  const int pages = (max(len, 0) + 15) / 16 - from;
-  return max((max(pages, 0) + records - 1) / records, kRestMinPages);
-}
-
 // out[d] = bf16( v_scale * sum_s e^(m_s - M) o_s[d] / sum_s e^(m_s - M) l_s ) of head h of the
 // group, over ns records of `base`: record s for s < np, s + gap behind it.  One workgroup: 32
 // lanes hold the head's dims, kMergeSets such sets take the records in turn (their loads are then
@@ -87,6 +79,35 @@ __device__ __forceinline__ void merge_records(const float* __restrict__ base, in
   orow[0] = o2.x;                                  // (out is 4-byte aligned)
   orow[1] = o2.y;
 }
+
+// The same with 32 lanes (lane: threadIdx.x % 32) alone, for a few records.
+template <int kG>
+__device__ __forceinline__ void merge_few_records(const float* __restrict__ base, int ns, int np, int gap, int h,
+                                                  const float* __restrict__ v_scale, uint16_t* __restrict__ out) {
+  const int d = 4 * (threadIdx.x & 31);
+  float m = kNoScore, l = 0.0f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = 0; s < ns; ++s) {
+    const float* r = base + (int64_t)(s < np ? s : s + gap) * partial_floats<kG>();
+    const float ms = r[rec_m<kG>() + h], ls = r[rec_l<kG>() + h];
+    const float4 o = *reinterpret_cast<const float4*>(r + h * 128 + d);
+    const float mn = fmaxf(m, ms), f = expf(m - mn), w = expf(ms - mn);
+    l = l * f + ls * w;
+    a.x = a.x * f + o.x * w;
+    a.y = a.y * f + o.y * w;
+    a.z = a.z * f + o.z * w;
+    a.w = a.w * f + o.w * w;
+    m = mn;
+  }
+  const float f = ns > 0 ? v_scale[0] / l : 0.0f;
+  uint32_t* orow = reinterpret_cast<uint32_t*>(out + d);
+  orow[0] = f32_to_bf16_rne(a.x * f) | (f32_to_bf16_rne(a.y * f) << 16);
+  orow[1] = f32_to_bf16_rne(a.z * f) | (f32_to_bf16_rne(a.w * f) << 16);
+}
+
+// Records up to which 32 lanes join them alone.
+constexpr int kFewRecords = 8;
 
 }  // namespace
 }  // namespace fp8rl

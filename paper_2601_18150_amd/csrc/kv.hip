@@ -370,8 +370,8 @@ __device__ __forceinline__ void attn_decode_split_of(
     const typename CacheElem<kFp8>::T* __restrict__ vcache, int64_t num_blocks,
     const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens, int max_seq_len,
     const float* __restrict__ k_scale, const float* __restrict__ v_scale, float sm_scale, int kv_heads,
-    int first_page, int split_pages, int records, int first_record, bool direct, float* __restrict__ partial,
-    uint16_t* __restrict__ out, uint8_t* lds) {
+    int split_pages, int max_splits, float* __restrict__ partial, uint16_t* __restrict__ out,
+    uint8_t* lds) {
   constexpr int kElem = kFp8 ? 1 : 2;
   constexpr int kHalf = AttnLds<kG, kFp8>::kHalf;
   constexpr int kDepth = kRingDepth;
@@ -385,7 +385,7 @@ __device__ __forceinline__ void attn_decode_split_of(
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
   const int g = lane >> 4, j = lane & 15;
-  const int p0 = first_page + split * split_pages;
+  const int p0 = split * split_pages;
   const int32_t* table = block_table + (int64_t)b * max_blocks;
   auto page_id = [&](int i) {                             // a bad entry reads a wrong page, never outside
     const int blk = table[min(p0 + wave + i * kWaves, max_blocks - 1)];
@@ -398,7 +398,7 @@ __device__ __forceinline__ void attn_decode_split_of(
   const int p1 = min((n + kPage - 1) / kPage, p0 + split_pages);
   uint16_t* orow = out + ((int64_t)b * kv_heads + kvh) * kG * kDim;
   if (p0 >= p1) {                                         // (uniform over the workgroup)
-    if (direct)                                           // an empty sequence gives 0
+    if (max_splits == 1)                                  // an empty sequence gives 0
       for (int i = threadIdx.x; i < kG * kDim / 2; i += 256) reinterpret_cast<uint32_t*>(orow)[i] = 0u;
     return;
   }
@@ -554,7 +554,7 @@ __device__ __forceinline__ void attn_decode_split_of(
     }
   }
   __syncthreads();
-  float* rec = partial + (((int64_t)b * kv_heads + kvh) * records + first_record + split) * partial_floats<kG>();
+  float* rec = partial + (((int64_t)b * kv_heads + kvh) * max_splits + split) * partial_floats<kG>();
   for (int e = threadIdx.x; e < kG * kDim / 2; e += 256) {
     const int head = e / (kDim / 2), d = 2 * (e % (kDim / 2));
     float mm = kNoScore;
@@ -573,7 +573,7 @@ __device__ __forceinline__ void attn_decode_split_of(
       a0 += c[head * kDim + d] * f[w];
       a1 += c[head * kDim + d + 1] * f[w];
     }
-    if (direct) {                                // the whole sequence: the output itself
+    if (max_splits == 1) {                       // the whole sequence: the output itself
       const float f = (v_scale ? v_scale[0] : 1.0f) / ls;
       reinterpret_cast<uint32_t*>(orow)[e] = f32_to_bf16_rne(a0 * f) | (f32_to_bf16_rne(a1 * f) << 16);
     } else {
@@ -595,8 +595,7 @@ __global__ __launch_bounds__(kMfmaBounds) void attn_decode_kernel(
     int split_pages, int max_splits, float* __restrict__ partial, uint16_t* __restrict__ out) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[AttnLds<kG, kFp8>::kBytes];
   attn_decode_split_of<kG, kFp8>(q, kcache, vcache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale,
-                                 v_scale, sm_scale, kv_heads, 0, split_pages, max_splits, 0, max_splits == 1, partial,
-                                 out, lds);
+                                 v_scale, sm_scale, kv_heads, split_pages, max_splits, partial, out, lds);
 }
 
 // out[b][head] = the sequence's split records joined (attn_merge.hpp), one workgroup per (head,
@@ -611,24 +610,6 @@ __global__ __launch_bounds__(32 * kMergeSets) void attn_merge_kernel(
   const int ns = min(max_splits, (max(n, 0) + split_pages * kPage - 1) / (split_pages * kPage));
   const float* base = partial + ((int64_t)b * kv_heads + kvh) * max_splits * partial_floats<kG>();
   merge_records<kG>(base, ns, ns, 0, h, v_scale, out + ((int64_t)b * kv_heads * kG + head) * kDim);
-}
-
-// One layer of a batch whose sequences have a first part attended to elsewhere: workgroup (kv
-// head, sequence, split) takes its share of the pages from first_page[b] on, divided evenly over
-// the records that the sequence has room for, and leaves record first_record + split.
-template <int kG>
-__global__ __launch_bounds__(kMfmaBounds) void attn_decode_rest_kernel(
-    const uint16_t* __restrict__ q, const uint8_t* __restrict__ kcache, const uint8_t* __restrict__ vcache,
-    int64_t num_blocks, const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens,
-    int max_seq_len, const float* __restrict__ k_scale, const float* __restrict__ v_scale, float sm_scale, int kv_heads,
-    const int32_t* __restrict__ first_page, int first_record, int records, float* __restrict__ partial) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[AttnLds<kG, true>::kBytes];
-  const int b = blockIdx.y;
-  const int from = max(first_page[b], 0);
-  const int per = rest_split_pages(min(seq_lens[b], max_seq_len), from, (int)gridDim.z);
-  attn_decode_split_of<kG, true>(q, kcache, vcache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale,
-                                 v_scale, sm_scale, kv_heads, from, per, records, first_record, false, partial, nullptr,
-                                 lds);
 }
 
 }  // namespace
@@ -750,31 +731,6 @@ hipError_t launch_attention_decode(const uint16_t* q, const void* k_cache, const
   FP8RL_ATTN(8)
 #undef FP8RL_ATTN
   return hipErrorInvalidValue;
-}
-
-// Records per (sequence, kv head) for the parts behind a shared prefix, as a decode step's splits.
-int attn_rest_records(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_seq_len) {
-  return attn_plan(batch, kv_heads, group, max_seq_len).splits;
-}
-
-hipError_t launch_attention_decode_rest(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
-                                        int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
-                                        const int32_t* seq_lens, int64_t batch, int64_t group, int64_t kv_heads,
-                                        int64_t max_seq_len, const float* k_scale, const float* v_scale, float sm_scale,
-                                        const int32_t* first_page, int first_record, int records, float* partial,
-                                        hipStream_t stream) {
-  const dim3 grid((unsigned)kv_heads, (unsigned)batch, (unsigned)(records - first_record));
-#define FP8RL_REST(G)                                                                                              \
-  if (group == G)                                                                                                  \
-    hipLaunchKernelGGL((attn_decode_rest_kernel<G>), grid, dim3(256), 0, stream, q, k_cache, v_cache, num_blocks,  \
-                       block_table, (int)max_blocks, seq_lens, (int)max_seq_len, k_scale, v_scale, sm_scale,       \
-                       (int)kv_heads, first_page, first_record, records, partial);
-  FP8RL_REST(1)
-  FP8RL_REST(2)
-  FP8RL_REST(4)
-  FP8RL_REST(8)
-#undef FP8RL_REST
-  return hipGetLastError();
 }
 
 }  // namespace fp8rl

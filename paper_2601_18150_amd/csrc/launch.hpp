@@ -120,17 +120,6 @@ hipError_t launch_attention_decode(const uint16_t* q, const void* k_cache, const
                                    int64_t max_seq_len, const float* k_scale, const float* v_scale, float sm_scale,
                                    uint16_t* out, float* partial, hipStream_t stream);
 
-// The decode kernel over the pages from first_page[b] on alone (FP8 cache): records first_record ..
-// records - 1 of each (sequence, kv head), nothing of `out`.
-int attn_rest_records(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_seq_len);
-
-hipError_t launch_attention_decode_rest(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
-                                        int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,
-                                        const int32_t* seq_lens, int64_t batch, int64_t group, int64_t kv_heads,
-                                        int64_t max_seq_len, const float* k_scale, const float* v_scale, float sm_scale,
-                                        const int32_t* first_page, int first_record, int records, float* partial,
-                                        hipStream_t stream);
-
 // Attention of whole prompts and of chunks against the FP8 cache.
 struct PromptSplit {
   int splits, split_keys;
@@ -139,7 +128,7 @@ struct PromptSplit {
 PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len);
 
 // workgroups per split
-int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads);
+int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, bool fp8);
 
 hipError_t launch_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t* k, int64_t ld_k,
                                         const uint16_t* v, int64_t ld_v, const int32_t* cu_seqlens, int64_t batch,
@@ -162,7 +151,9 @@ struct SharedSplit {
 SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,
                               int64_t max_seq_len);
 
-int64_t attn_shared_workgroups(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads);
+// workgroups of the whole call
+int64_t attn_shared_workgroups(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,
+                               int64_t max_seq_len);
 
 hipError_t launch_attention_decode_shared(const uint16_t* q, const uint8_t* k_cache, const uint8_t* v_cache,
                                           int64_t num_blocks, const int32_t* block_table, int64_t max_blocks,

@@ -12,6 +12,7 @@
 
 #include "attn_core.hpp"
 #include "attn_merge.hpp"
+#include "attn_stream.hpp"
 #include "launch.hpp"
 
 namespace fp8rl {
@@ -41,23 +42,30 @@ struct PromptArgs {
   int32_t* counts;             // records of each token
 };
 
+constexpr int kPromptSmall = 64;   // rows of a run up to which it takes tiles of 32 (FP8 cache)
+
 template <bool kFp8>
 __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_kernel(const PromptArgs p) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kTileBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t lds_values[kTileBytes];
+  // (FP8: the rings of the small tiles)
+  __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kFp8 ? kRingBytes : kTileBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_values[kFp8 ? kRingBytes : kTileBytes];
   const TileLds lds{lds_keys, lds_values};
   const int kvh = blockIdx.x % p.kv_heads, tiles = gridDim.x / p.kv_heads;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TileOf at;
-  if (!find_tile(p.cu_seqlens, p.batch, p.total, p.group_log2, tiles - 1 - (int)(blockIdx.x / p.kv_heads), at)) return;
+  if (!find_tile(p.cu_seqlens, p.batch, p.total, p.group_log2, kFp8 ? kPromptSmall : 0,
+                 tiles - 1 - (int)(blockIdx.x / p.kv_heads), at))
+    return;
   at.to_scalars();
   const int group = 1 << p.group_log2;
   const int len = kFp8 ? min(max(p.seq_lens[at.b], 0), p.max_seq_len) : at.n;
   const int first = len - at.n;                         // position of the call's first token of the sequence
-  const int rows = at.n << p.group_log2, row0 = at.index * kAttnRows;
+  const int rows = at.n << p.group_log2;
+  const bool small = kFp8 && rows <= kPromptSmall;
+  const int tile = small ? kStreamRows : kAttnRows, row0 = at.index * tile;
   auto position = [&](int r) { return first + (min(r, rows - 1) >> p.group_log2); };
-  const int r = row0 + kRowsPerWave * wave + (lane & 31);
+  const int r = row0 + (small ? 0 : kRowsPerWave * wave) + (lane & 31);
   const int token = at.first + (min(r, rows - 1) >> p.group_log2);
   const int head = kvh * group + (min(r, rows - 1) & (group - 1));
   AttnRow row;
@@ -66,21 +74,48 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   row.wave_last = position(row0 + kRowsPerWave * wave + kRowsPerWave - 1);
   const int split = blockIdx.y;
   const int begin = split * p.split_keys;
-  const int end = min(position(row0 + kAttnRows - 1) + 1, p.splits > 1 ? begin + p.split_keys : 0x7FFFFFFF);
+  const int end = min(position(row0 + tile - 1) + 1, p.splits > 1 ? begin + p.split_keys : 0x7FFFFFFF);
   if (p.splits > 1 && split == 0 && kvh == 0 && (r & (group - 1)) == 0 && r < rows && lane < 32)
     p.counts[token] = row.limit < 0 ? 0 : row.limit / p.split_keys + 1;
   if (begin >= end && p.splits > 1) return;
   row.all_limit = min(position(row0), end - 1);
 
+  const float sscale = (kFp8 ? p.k_scale[0] : 1.0f) * p.sm_scale;
+  const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
+  const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;
+  auto record = [&](int tok) { return p.records + (((int64_t)tok * p.kv_heads + kvh) * p.splits + split) * floats; };
+  const PagedKv pages{static_cast<const uint8_t*>(p.k), static_cast<const uint8_t*>(p.v),
+                      p.block_table + (int64_t)at.b * p.max_blocks, p.num_blocks, p.max_blocks, p.kv_heads, kvh};
+  if (kFp8 && small) {
+    __shared__ StreamStats stats;
+    AttnAcc part_acc;                                   // (nothing that the large tiles' loop has in registers)
+    attn_init(part_acc);
+    row.limit = min(row.limit, end - 1);                // (the next split's keys are its own)
+    bf16x8 part_q[8];
+    attn_load_q(row, part_q);
+    attn_stream(part_acc, part_q, row, begin, end, c, pages, len, lds);
+    stream_join(part_acc, c, lds, stats, [&](int i, int part, const float4 (&o)[4], float m, float l) {
+      const int ri = row0 + i, tok = at.first + (ri >> p.group_log2), hd = ri & (group - 1);
+      if (ri >= rows) return;
+      if (p.splits > 1) {
+        float* rec = record(tok);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) *reinterpret_cast<float4*>(rec + hd * kHeadDim + 16 * part + 4 * n) = o[n];
+        if (part == 0) {
+          rec[group * kHeadDim + hd] = fmaxf(m * sscale, kNoScore);
+          rec[group * kHeadDim + group + hd] = l;
+        }
+      } else {
+        store16_bf16(o, l == 0.0f ? 0.0f : p.v_scale[0] / l, p.out + tok * p.ld_out + (kvh * group + hd) * kHeadDim + 16 * part);
+      }
+    });
+    return;
+  }
   AttnAcc acc;
   attn_init(acc);
   bf16x8 q[8];
   attn_load_q(row, q);
-  const float sscale = (kFp8 ? p.k_scale[0] : 1.0f) * p.sm_scale;
-  const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
   if constexpr (kFp8) {
-    const PagedKv pages{static_cast<const uint8_t*>(p.k), static_cast<const uint8_t*>(p.v),
-                        p.block_table + (int64_t)at.b * p.max_blocks, p.num_blocks, p.max_blocks, p.kv_heads, kvh};
     attn_run_fp8(acc, q, row, begin, end, c, pages, len, lds);
   } else {
     const Bf16Rows<false> k(static_cast<const uint16_t*>(p.k) + at.first * p.ld_k + kvh * kHeadDim, p.ld_k, len);
@@ -90,8 +125,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   const float l = half_sum(acc.l);
   const bool valid = r < rows;
   if (p.splits > 1) {
-    const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;
-    float* rec = p.records + (((int64_t)token * p.kv_heads + kvh) * p.splits + split) * floats;
+    float* rec = record(token);
     const int h = head & (group - 1);
     attn_store_f32(acc, rec + h * kHeadDim, valid);
     if (valid && lane < 32) {
@@ -104,24 +138,34 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   }
 }
 
-// One workgroup per (query head, token): the token's records joined.
-template <int kG>
-__global__ __launch_bounds__(32 * kMergeSets) void attn_prompt_merge_kernel(const PromptArgs p) {
-  const int head = blockIdx.x, token = blockIdx.y + blockIdx.z * 32768;
+// A token's records joined: kFew: eight (token, query head) pairs a workgroup, 32 lanes each; otherwise one.
+template <int kG, bool kFew>
+__global__ __launch_bounds__(kFew ? 256 : 32 * kMergeSets) void attn_prompt_merge_kernel(const PromptArgs p) {
+  const int64_t pair = kFew ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
+  const int heads = p.kv_heads * kG;
+  const int token = (int)(pair / heads), head = (int)(pair % heads);
   const int lo = min(max(p.cu_seqlens[0], 0), p.total), hi = min(max(p.cu_seqlens[p.batch], 0), p.total);
   if (token < lo || token >= hi) return;                 // rows of no sequence stay as they are
   const int kvh = head / kG, h = head % kG;
   const int ns = min(p.counts[token], p.splits);
   const float* base = p.records + ((int64_t)token * p.kv_heads + kvh) * p.splits * partial_floats<kG>();
-  merge_records<kG>(base, ns, ns, 0, h, p.v_scale, p.out + token * p.ld_out + head * kHeadDim);
+  uint16_t* out = p.out + token * p.ld_out + head * kHeadDim;
+  if constexpr (kFew)
+    merge_few_records<kG>(base, ns, ns, 0, h, p.v_scale, out);
+  else
+    merge_records<kG>(base, ns, ns, 0, h, p.v_scale, out);
 }
 
 }  // namespace
 
+int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, bool fp8) {
+  return attn_tile_bound(total * group, batch < total ? batch : total, fp8 ? kPromptSmall : 0) * kv_heads;
+}
+
 // Splits of the keys where the tiles alone are too few for the 512 workgroups that the chip holds:
 // as many as fill them, of at least 256 keys each.
 PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len) {
-  const int64_t wgs = attn_tile_bound(total * group, batch < total ? batch : total) * kv_heads;
+  const int64_t wgs = attn_tile_guess(total * group, batch < total ? batch : total, kPromptSmall) * kv_heads;
   int64_t splits = wgs > 0 ? (512 + wgs - 1) / wgs : 1;
   int64_t keys = (max_seq_len + splits - 1) / splits;
   keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;
@@ -134,10 +178,6 @@ PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64
   return s;
 }
 
-int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads) {
-  return attn_tile_bound(total * group, batch < total ? batch : total) * kv_heads;
-}
-
 hipError_t launch_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t* k, int64_t ld_k,
                                         const uint16_t* v, int64_t ld_v, const int32_t* cu_seqlens, int64_t batch,
                                         int64_t total, int64_t q_heads, int64_t kv_heads, float sm_scale, uint16_t* out,
@@ -147,7 +187,7 @@ hipError_t launch_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const u
   p.q = q, p.ld_q = ld_q, p.k = k, p.ld_k = ld_k, p.v = v, p.ld_v = ld_v;
   p.cu_seqlens = cu_seqlens, p.batch = (int)batch, p.total = (int)total, p.kv_heads = (int)kv_heads;
   p.group_log2 = group_log2_of(group), p.sm_scale = sm_scale, p.out = out, p.ld_out = ld_out, p.splits = 1;
-  hipLaunchKernelGGL((attn_prompt_kernel<false>), dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads)),
+  hipLaunchKernelGGL((attn_prompt_kernel<false>), dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads, false)),
                      dim3(64 * kAttnWaves), 0, stream, p);
   return hipGetLastError();
 }
@@ -170,16 +210,22 @@ hipError_t launch_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const 
   p.records = workspace;
   p.counts = reinterpret_cast<int32_t*>(workspace + total * kv_heads * sp.splits * sp.partial_floats);
   hipLaunchKernelGGL((attn_prompt_kernel<true>),
-                     dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads), (unsigned)sp.splits),
+                     dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads, true), (unsigned)sp.splits),
                      dim3(64 * kAttnWaves), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.splits == 1) return e;
-  const dim3 grid((unsigned)q_heads, (unsigned)(total < 32768 ? total : 32768), (unsigned)((total + 32767) / 32768));
-  const dim3 block(32 * kMergeSets);
-  if (group == 1) hipLaunchKernelGGL((attn_prompt_merge_kernel<1>), grid, block, 0, stream, p);
-  if (group == 2) hipLaunchKernelGGL((attn_prompt_merge_kernel<2>), grid, block, 0, stream, p);
-  if (group == 4) hipLaunchKernelGGL((attn_prompt_merge_kernel<4>), grid, block, 0, stream, p);
-  if (group == 8) hipLaunchKernelGGL((attn_prompt_merge_kernel<8>), grid, block, 0, stream, p);
+  const bool few = sp.splits <= kFewRecords;
+  const dim3 grid((unsigned)(few ? (total * q_heads + 7) / 8 : total * q_heads)), block(few ? 256 : 32 * kMergeSets);
+#define FP8RL_MERGE(G)                                                                                            \
+  if (group == G) {                                                                                               \
+    if (few) hipLaunchKernelGGL((attn_prompt_merge_kernel<G, true>), grid, block, 0, stream, p);                  \
+    else hipLaunchKernelGGL((attn_prompt_merge_kernel<G, false>), grid, block, 0, stream, p);                     \
+  }
+  FP8RL_MERGE(1)
+  FP8RL_MERGE(2)
+  FP8RL_MERGE(4)
+  FP8RL_MERGE(8)
+#undef FP8RL_MERGE
   return hipGetLastError();
 }
 
