@@ -646,20 +646,25 @@ def _head_rows(x: torch.Tensor, what: str):
     if x.dtype != torch.bfloat16 or x.dim() != 3:
         raise TypeError(f"{what} must be bfloat16 [tokens][heads][head_dim]")
     t, h, d = x.shape
-    if t > 0 and h > 0 and ((d > 1 and x.stride(2) != 1) or (h > 1 and x.stride(1) != d)):
-        raise ValueError(f"the heads of a token of {what} must lie side by side")
-    return x.stride(0) if t > 1 else h * d
+    pitch, head, col = x.stride()
+    if (d > 1 and col != 1) or (h > 1 and head != d):
+        if t > 0 and h > 0:
+            raise ValueError(f"the heads of a token of {what} must lie side by side")
+    return pitch if t > 1 else h * d
 
 
 def _here(*ts):
     """One HIP device for all, and the current one: kernels start there, on its current stream."""
-    _dev(*ts)
-    if ts[0].get_device() != torch._C._cuda_getDevice():
+    dev = ts[0].get_device()                               # (-1 for a host tensor)
+    if dev < 0 or set(map(torch.Tensor.get_device, ts)) != {dev}:
+        _dev(*ts)
+        raise ValueError("fp8rl tensors must live on a HIP device")
+    if dev != torch._C._cuda_getDevice():
         raise ValueError("fp8rl tensors must live on the current device")
 
 
 def _i32(x: torch.Tensor, n, what: str):
-    if x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous() or (n is not None and x.numel() != n):
+    if x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous() or (n is not None and x.shape[0] != n):
         raise ValueError(f"{what} must be contiguous int32 [{'n' if n is None else n}]")
 
 
@@ -668,12 +673,12 @@ def _paged(k_cache, v_cache, block_table):
     k_cache, v_cache = _u8(k_cache), _u8(v_cache)
     if k_cache.dim() < 2 or not (k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise ValueError("the caches must be contiguous [num_blocks][kv_heads][..]")
-    if k_cache.shape[:2] != v_cache.shape[:2] or k_cache.numel() != v_cache.numel() or \
-            k_cache.numel() != k_cache.shape[0] * k_cache.shape[1] * 2048:
+    blocks, kv_heads = k_cache.shape[:2]
+    if v_cache.shape[:2] != (blocks, kv_heads) or not k_cache.numel() == v_cache.numel() == blocks * kv_heads * 2048:
         raise ValueError("the caches must hold 16 x 128 codes per block and kv head")
     if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
         raise ValueError("block_table must be contiguous int32 [batch][max_blocks]")
-    return k_cache, v_cache, k_cache.shape[0], k_cache.shape[1]
+    return k_cache, v_cache, blocks, kv_heads
 
 
 def _scale1(*scales):
@@ -690,9 +695,10 @@ def _out_rows(out, q):
     return out
 
 
-def _workspace(workspace, need: int, device):
+def _workspace(workspace, device, size, *args):
+    """The caller's workspace (whose size the library checks), or one of size(*args) bytes."""
     if workspace is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        return torch.empty(max(size(*args), 16), dtype=torch.uint8, device=device)
     if not workspace.is_contiguous():
         raise ValueError("the workspace must be contiguous")
     return workspace
@@ -741,8 +747,8 @@ def fp8rl_attention_prompt_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, v_cache
     _scale1(k_scale, v_scale)
     out = _out_rows(out, q)
     ld_out = _head_rows(out, "out")
-    need = fp8rl_attention_prompt_workspace_size(batch, total, q_heads, kv_heads, int(max_seq_len))
-    workspace = _workspace(workspace, need, q.device)
+    workspace = _workspace(workspace, q.device, fp8rl_attention_prompt_workspace_size, batch, total, q_heads, kv_heads,
+                           int(max_seq_len))
     _here(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, out, workspace)
     st = load().fp8rl_attention_prompt_fp8kv(q.data_ptr(), ld_q, k_cache.data_ptr(), v_cache.data_ptr(), num_blocks,
                                              block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(),
@@ -784,9 +790,8 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
     out = _out_rows(out, q)
     if out.dtype != torch.bfloat16 or not out.is_contiguous():
         raise ValueError("out must be contiguous bfloat16")
-    need = fp8rl_attention_decode_shared_workspace_size(batch, groups, q_heads, kv_heads, int(max_prefix_len),
-                                                        int(max_seq_len))
-    workspace = _workspace(workspace, need, q.device)
+    workspace = _workspace(workspace, q.device, fp8rl_attention_decode_shared_workspace_size, batch, groups, q_heads,
+                           kv_heads, int(max_prefix_len), int(max_seq_len))
     _here(q, k_cache, v_cache, block_table, seq_lens, group_offsets, prefix_lens, k_scale, v_scale, out, workspace)
     st = load().fp8rl_attention_decode_shared_fp8kv(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_blocks, block_table.data_ptr(), block_table.shape[1],
@@ -799,15 +804,17 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
 
 def _cache_list(caches):
     """(ctypes array of base pointers, count, bytes per block, blocks) of caches [num_blocks][..] of one block size."""
-    caches = list(caches)
     if not caches:
         raise ValueError("at least one cache")
-    blocks = caches[0].shape[0] if caches[0].dim() else 0
-    size = caches[0].numel() * caches[0].element_size()
-    for c in caches:
-        if not c.is_contiguous() or c.dim() < 2 or c.shape[0] != blocks or c.numel() * c.element_size() != size:
-            raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
-    return (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches]), len(caches), size // max(blocks, 1), blocks
+    first, n = caches[0], len(caches)
+    shape = first.shape
+    blocks, size = (shape[0] if shape else 0), first.numel() * first.element_size()
+    # (most often all are alike, which is tested without a Python step for each: a model has a hundred)
+    alike = all(map(shape.__eq__, [c.shape for c in caches])) and len(set(map(torch.Tensor.element_size, caches))) == 1
+    if not all(map(torch.Tensor.is_contiguous, caches)) or len(shape) < 2 or not (alike or all(
+            c.dim() > 1 and c.shape[0] == blocks and c.numel() * c.element_size() == size for c in caches)):
+        raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
+    return (ctypes.c_void_p * n)(*map(torch.Tensor.data_ptr, caches)), n, size // max(blocks, 1), blocks
 
 
 def _table(block_table, seq_lens, block_refs, blocks=None):
@@ -869,7 +876,7 @@ def fp8rl_kv_compact(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, 
     if live is None:
         live = torch.empty(1, dtype=torch.int32, device=dev)
     _i32(live, 1, "live")
-    workspace = _workspace(workspace, fp8rl_kv_compact_workspace_size(blocks), dev)
+    workspace = _workspace(workspace, dev, fp8rl_kv_compact_workspace_size, blocks)
     _here(*caches, block_table, seq_lens, block_refs, live, workspace)
     _check("fp8rl_kv_compact", load().fp8rl_kv_compact(
         ptrs, n, size, blocks, block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(),

@@ -22,28 +22,49 @@ struct Caches {
 
 __device__ __forceinline__ bool in_cache(const Caches& c, int blk) { return blk >= 0 && (int64_t)blk < c.num_blocks; }
 
-// Block dst = block src of cache i, by the whole workgroup, four loads in flight a thread.
-__device__ __forceinline__ void copy_block(const Caches& c, int i, int src, int dst) {
-  const uint4* s = reinterpret_cast<const uint4*>(c.base[i] + src * c.block_bytes);
-  uint4* d = reinterpret_cast<uint4*>(c.base[i] + dst * c.block_bytes);
-  const int64_t n = c.block_bytes / 16;
-  for (int64_t at = threadIdx.x; at < n; at += 4 * kThreads) {
-    uint4 v[4];
+// A workgroup copies one block of several caches, kSlices slices of 4 KiB all told: every load is on its way
+// before the first is stored, which with fewer bytes in flight a CU are two latencies in a row (1264 blocks of 8
+// KiB in 24 caches, 498 MB read and written: 170 us for a cache at a time, XX us so).
+constexpr int kSlices = 8;
+constexpr int kSliceBytes = 16 * kThreads;
+
+__host__ __device__ inline int64_t slices_of(int64_t block_bytes) { return (block_bytes + kSliceBytes - 1) / kSliceBytes; }
+// caches whose blocks a workgroup copies together
+__host__ __device__ inline int caches_per_group(int64_t block_bytes) {
+  const int64_t s = slices_of(block_bytes);
+  return s >= kSlices ? 1 : s < 1 ? kSlices : (int)(kSlices / s);
+}
+
+// Block dst = block src of the caches of column x.
+__device__ __forceinline__ void copy_block(const Caches& c, int x, int count, int src, int dst) {
+  const int per = caches_per_group(c.block_bytes), spb = (int)slices_of(c.block_bytes);
+  const int first = x * per, total = min(per, count - first) * spb;
+  const int64_t lane = threadIdx.x * 16;
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  for (int s0 = 0; s0 < total; s0 += kSlices) {
+    u32x4 v[kSlices];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (at + u * kThreads < n) v[u] = s[at + u * kThreads];
+    for (int u = 0; u < kSlices; ++u) {                    // (past the end: the last slice, the last bytes again)
+      const int s = min(s0 + u, total - 1), i = s / spb;   // (uniform)
+      const int64_t off = min((int64_t)(s - i * spb) * kSliceBytes + lane, c.block_bytes - 16);
+      v[u] = *reinterpret_cast<const u32x4*>(c.base[first + i] + src * c.block_bytes + off);
+    }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (at + u * kThreads < n) d[at + u * kThreads] = v[u];
+    for (int u = 0; u < kSlices; ++u) {
+      const int s = s0 + u, i = s / spb;
+      const int64_t off = (int64_t)(s - i * spb) * kSliceBytes + lane;
+      if (s < total && off < c.block_bytes)
+        *reinterpret_cast<u32x4*>(c.base[first + i] + dst * c.block_bytes + off) = v[u];
+    }
   }
 }
 
-// Workgroup (cache, pair).
-__global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const Caches c, const int32_t* __restrict__ src,
+// Workgroup (column of caches, pair).
+__global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const Caches c, int caches, const int32_t* __restrict__ src,
                                                               const int32_t* __restrict__ dst, int64_t count) {
   for (int64_t i = blockIdx.y; i < count; i += gridDim.y) {
     const int s = src[i], d = dst[i];
-    if (in_cache(c, s) && in_cache(c, d) && s != d) copy_block(c, blockIdx.x, s, d);
+    if (in_cache(c, s) && in_cache(c, d) && s != d) copy_block(c, blockIdx.x, caches, s, d);
   }
 }
 
@@ -59,10 +80,10 @@ struct ForkArgs {
   int64_t count;
 };
 
-// Workgroup (cache, fork): the parent's last page, where it is partly filled, copied to the child's
-// own; cache 0's also writes the child's row, length and the counts (sums of whole numbers: the
+// Workgroup (column of caches, fork): the parent's last page, where it is partly filled, copied to the child's
+// own; column 0's also writes the child's row, length and the counts (sums of whole numbers: the
 // order in which forks of one parent add to them does not show).
-__global__ __launch_bounds__(kThreads) void fork_kernel(const Caches c, const ForkArgs p, bool tables) {
+__global__ __launch_bounds__(kThreads) void fork_kernel(const Caches c, int caches, const ForkArgs p, bool tables) {
   for (int64_t i = blockIdx.y; i < p.count; i += gridDim.y) {
     const int parent = p.parents[i], child = p.children[i];
     if (parent < 0 || parent >= p.rows || child < 0 || child >= p.rows || parent == child) continue;
@@ -75,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(const Caches c, const Fo
       src = from[whole];
       dst = p.new_blocks[i];
       if (!in_cache(c, src) || !in_cache(c, dst)) continue;            // no page for it: no fork
-      if (src != dst) copy_block(c, blockIdx.x, src, dst);
+      if (src != dst) copy_block(c, blockIdx.x, caches, src, dst);
     }
     if (!tables || blockIdx.x != 0) continue;
     int32_t* to = p.table + child * (int64_t)p.max_blocks;
@@ -203,15 +224,15 @@ struct CompactArgs {
   CompactPlan plan;
 };
 
-// Workgroup (cache, k), k + gridDim.y, ..: a move; the column behind the caches' (`tables`): the
+// Workgroup (column of caches, k), k + gridDim.y, ..: a move; the column behind them (`tables`): the
 // counts of the blocks that moved, and the rows that name them.
-__global__ __launch_bounds__(kThreads) void move_kernel(const Caches c, int count, const CompactArgs p, bool tables) {
+__global__ __launch_bounds__(kThreads) void move_kernel(const Caches c, int caches, int columns, const CompactArgs p) {
   const int moves = *p.plan.moves;
-  if ((int)blockIdx.x < count) {
-    for (int k = blockIdx.y; k < moves; k += gridDim.y) copy_block(c, blockIdx.x, p.plan.movers[k], p.plan.holes[k]);
+  if ((int)blockIdx.x < columns) {
+    for (int k = blockIdx.y; k < moves; k += gridDim.y)
+      copy_block(c, blockIdx.x, caches, p.plan.movers[k], p.plan.holes[k]);
     return;
   }
-  if (!tables) return;
   for (int64_t k = (int64_t)blockIdx.y * kThreads + threadIdx.x; k < moves; k += (int64_t)gridDim.y * kThreads) {
     const int from = p.plan.movers[k];
     p.refs[p.plan.holes[k]] = p.refs[from];
@@ -251,6 +272,11 @@ hipError_t each_launch(void* const* caches, int64_t num_caches, int64_t block_by
   return hipSuccess;
 }
 
+unsigned columns_of(unsigned caches, int64_t block_bytes) {
+  const unsigned per = (unsigned)caches_per_group(block_bytes);
+  return (caches + per - 1) / per;
+}
+
 unsigned grid_y(int64_t n) { return (unsigned)(n < 32768 ? n : 32768); }
 
 }  // namespace
@@ -258,7 +284,8 @@ unsigned grid_y(int64_t n) { return (unsigned)(n < 32768 ? n : 32768); }
 hipError_t launch_kv_copy_blocks(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,
                                  const int32_t* src, const int32_t* dst, int64_t count, hipStream_t stream) {
   return each_launch(caches, num_caches, block_bytes, num_blocks, [&](const Caches& c, unsigned n, bool) {
-    hipLaunchKernelGGL(copy_blocks_kernel, dim3(n, grid_y(count)), dim3(kThreads), 0, stream, c, src, dst, count);
+    hipLaunchKernelGGL(copy_blocks_kernel, dim3(columns_of(n, block_bytes), grid_y(count)), dim3(kThreads), 0, stream, c,
+                       (int)n, src, dst, count);
   });
 }
 
@@ -267,7 +294,8 @@ hipError_t launch_kv_fork(void* const* caches, int64_t num_caches, int64_t block
                           const int32_t* children, const int32_t* new_blocks, int64_t count, hipStream_t stream) {
   const ForkArgs p{table, rows, (int)max_blocks, seq_lens, refs, parents, children, new_blocks, count};
   return each_launch(caches, num_caches, block_bytes, num_blocks, [&](const Caches& c, unsigned n, bool first) {
-    hipLaunchKernelGGL(fork_kernel, dim3(n, grid_y(count)), dim3(kThreads), 0, stream, c, p, first);
+    hipLaunchKernelGGL(fork_kernel, dim3(block_bytes > 0 ? columns_of(n, block_bytes) : 1, grid_y(count)), dim3(kThreads), 0,
+                       stream, c, (int)n, p, first);
   });
 }
 
@@ -304,7 +332,10 @@ hipError_t launch_kv_compact(void* const* caches, int64_t num_caches, int64_t bl
   const int64_t most = num_blocks / 2 > rows ? num_blocks / 2 : rows;
   const unsigned y = (unsigned)(most < 1 ? 1 : most < 1024 ? most : 1024);
   return each_launch(caches, num_caches, block_bytes, num_blocks, [&](const Caches& c, unsigned n, bool first) {
-    hipLaunchKernelGGL(move_kernel, dim3(n + (first ? 1 : 0), y), dim3(kThreads), 0, stream, c, (int)n, p, first);
+    const unsigned columns = block_bytes > 0 ? columns_of(n, block_bytes) : 0;
+    if (columns + first == 0) return;
+    hipLaunchKernelGGL(move_kernel, dim3(columns + (first ? 1 : 0), y), dim3(kThreads), 0, stream, c, (int)n, (int)columns,
+                       p);
   });
 }
 

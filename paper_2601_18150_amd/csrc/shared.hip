@@ -38,8 +38,8 @@ struct SharedArgs {
   int32_t* prefix;         // of each sequence: tokens of it that are read with its group's
 };
 
-// Pages per record of a sequence's own `pages`, divided over `records`; at least 512 tokens.
-constexpr int kOwnMinPages = 32;
+// Pages per record of a sequence's own `pages`, divided over `records`; at least 256 tokens.
+constexpr int kOwnMinPages = 16;
 __device__ __forceinline__ int own_split_pages(int pages, int records) {
   return max((max(pages, 0) + records - 1) / records, kOwnMinPages);
 }
@@ -207,19 +207,25 @@ __global__ __launch_bounds__(kFew ? 256 : 32 * kMergeSets) void attn_shared_merg
 
 }  // namespace
 
-// Records of a sequence and kv head: the prefix's keys are split where its row tiles alone are too
-// few for the 512 workgroups that the chip holds, 256 keys each at least; the rest where the sequences
-// are, 512 tokens each at least.
+// Records of a sequence and kv head.  The prefixes' keys are split where their tiles alone are few, 256 keys
+// each at least, so that there are about 256 workgroups of small tiles and 384 of large ones: the chip holds
+// 512, and what is left over goes to the sequences' own tokens, which are bound by reading, meanwhile (us for
+// 256 / 384 / 512: 16 x 16 sequences of 1800 + up to 2500 tokens, small tiles, 176 / 185 / 183; 4 x 32 of 18000
+// + up to 1500, large ones, 98 / 86 / 92).  Own tokens are split where the sequences are fewer than 1024, 256
+// tokens each at least (4 x 8 of 4000 + up to 3000 tokens, for 512 / 1024 / 2048 / 4096: 48 / 47 / 48 / 50 us;
+// 4 x 32 as above 92 / 92 / 94 / 107).
 SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,
                               int64_t max_seq_len) {
-  const int64_t wgs = attn_tile_guess(batch * group, groups < batch ? groups : batch, kSharedSmall) * kv_heads;
-  int64_t splits = wgs > 0 ? (512 + wgs - 1) / wgs : 1;
+  const int64_t runs = groups < batch ? groups : batch;
+  const int64_t wgs = attn_tile_guess(batch * group, runs, kSharedSmall) * kv_heads;
+  const int64_t target = batch * group <= runs * kSharedSmall ? 256 : 384;
+  int64_t splits = wgs > 0 ? (target + wgs - 1) / wgs : 1;
   int64_t keys = (max_prefix_len + splits - 1) / splits;
   keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;
   if (keys < 256) keys = 256;
   splits = (max_prefix_len + keys - 1) / keys;
   const int64_t pairs = batch * kv_heads;
-  int64_t own = (2048 + pairs - 1) / pairs;
+  int64_t own = (1024 + pairs - 1) / pairs;
   const int64_t most = (max_seq_len + kOwnMinPages * kPageTokens - 1) / (kOwnMinPages * kPageTokens);
   own = own > most ? most : own;
   SharedSplit s;
