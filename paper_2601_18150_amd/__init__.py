@@ -15,6 +15,8 @@ scales), section 2.1.2 (weights re-quantised at every RL step), section 2.1.4
 from __future__ import annotations
 
 import ctypes
+import itertools
+import operator
 import os
 
 import torch  # loads torch's HIP runtime first, so libfp8rl binds to that same runtime
@@ -687,18 +689,28 @@ def _scale1(*scales):
             raise ValueError("k_scale and v_scale must be fp32 [1]")
 
 
-def _out_rows(out, q):
+def _empty(shape, dtype, device, stream):
+    """Memory of the stream that the call runs on (the allocator gives it to others only behind that stream's work)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _out_rows(out, q, stream):
     if out is None:
-        return torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        return _empty(q.shape, torch.bfloat16, q.device, stream)
     if out.shape != q.shape:
         raise ValueError("out must have q's shape")
     return out
 
 
-def _workspace(workspace, device, size, *args):
+def _workspace(workspace, device, stream, size, *args):
     """The caller's workspace (whose size the library checks), or one of size(*args) bytes."""
     if workspace is None:
-        return torch.empty(max(size(*args), 16), dtype=torch.uint8, device=device)
+        return _empty((max(size(*args), 16),), torch.uint8, device, stream)
     if not workspace.is_contiguous():
         raise ValueError("the workspace must be contiguous")
     return workspace
@@ -717,7 +729,7 @@ def fp8rl_attention_prompt_bf16(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     _i32(cu_seqlens, None, "cu_seqlens")
     if cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens must have batch + 1 entries")
-    out = _out_rows(out, q)
+    out = _out_rows(out, q, stream)
     ld_out = _head_rows(out, "out")
     _here(q, k, v, cu_seqlens, out)
     st = load().fp8rl_attention_prompt_bf16(q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
@@ -745,9 +757,9 @@ def fp8rl_attention_prompt_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, v_cache
     _i32(seq_lens, batch, "seq_lens")
     _i32(cu_seqlens, batch + 1, "cu_seqlens")
     _scale1(k_scale, v_scale)
-    out = _out_rows(out, q)
+    out = _out_rows(out, q, stream)
     ld_out = _head_rows(out, "out")
-    workspace = _workspace(workspace, q.device, fp8rl_attention_prompt_workspace_size, batch, total, q_heads, kv_heads,
+    workspace = _workspace(workspace, q.device, stream, fp8rl_attention_prompt_workspace_size, batch, total, q_heads, kv_heads,
                            int(max_seq_len))
     _here(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, out, workspace)
     st = load().fp8rl_attention_prompt_fp8kv(q.data_ptr(), ld_q, k_cache.data_ptr(), v_cache.data_ptr(), num_blocks,
@@ -787,10 +799,10 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
     groups = prefix_lens.numel()
     _i32(group_offsets, groups + 1, "group_offsets")
     _scale1(k_scale, v_scale)
-    out = _out_rows(out, q)
+    out = _out_rows(out, q, stream)
     if out.dtype != torch.bfloat16 or not out.is_contiguous():
         raise ValueError("out must be contiguous bfloat16")
-    workspace = _workspace(workspace, q.device, fp8rl_attention_decode_shared_workspace_size, batch, groups, q_heads,
+    workspace = _workspace(workspace, q.device, stream, fp8rl_attention_decode_shared_workspace_size, batch, groups, q_heads,
                            kv_heads, int(max_prefix_len), int(max_seq_len))
     _here(q, k_cache, v_cache, block_table, seq_lens, group_offsets, prefix_lens, k_scale, v_scale, out, workspace)
     st = load().fp8rl_attention_decode_shared_fp8kv(
@@ -807,12 +819,11 @@ def _cache_list(caches):
     if not caches:
         raise ValueError("at least one cache")
     first, n = caches[0], len(caches)
-    shape = first.shape
-    blocks, size = (shape[0] if shape else 0), first.numel() * first.element_size()
-    # (most often all are alike, which is tested without a Python step for each: a model has a hundred)
-    alike = all(map(shape.__eq__, [c.shape for c in caches])) and len(set(map(torch.Tensor.element_size, caches))) == 1
-    if not all(map(torch.Tensor.is_contiguous, caches)) or len(shape) < 2 or not (alike or all(
-            c.dim() > 1 and c.shape[0] == blocks and c.numel() * c.element_size() == size for c in caches)):
+    blocks, size = (first.shape[0] if first.dim() > 1 else -1), first.nbytes
+    # (a model has a hundred caches: no Python step for each)
+    if blocks < 0 or set(map(torch.Tensor.size, caches, itertools.repeat(0))) != {blocks} or \
+            set(map(operator.attrgetter("nbytes"), caches)) != {size} or \
+            not all(map(torch.Tensor.is_contiguous, caches)):
         raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
     return (ctypes.c_void_p * n)(*map(torch.Tensor.data_ptr, caches)), n, size // max(blocks, 1), blocks
 
@@ -874,9 +885,9 @@ def fp8rl_kv_compact(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, 
     _table(block_table, seq_lens, block_refs, blocks)
     dev = block_table.device
     if live is None:
-        live = torch.empty(1, dtype=torch.int32, device=dev)
+        live = _empty((1,), torch.int32, dev, stream)
     _i32(live, 1, "live")
-    workspace = _workspace(workspace, dev, fp8rl_kv_compact_workspace_size, blocks)
+    workspace = _workspace(workspace, dev, stream, fp8rl_kv_compact_workspace_size, blocks)
     _here(*caches, block_table, seq_lens, block_refs, live, workspace)
     _check("fp8rl_kv_compact", load().fp8rl_kv_compact(
         ptrs, n, size, blocks, block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(),

@@ -1,0 +1,130 @@
+"""Attention against the cache where it changes its way: rows on both sides of a tile, shares of pages that end inside a
+chunk of keys, caches past 4 GiB, streams other than the current one, two calls at once."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention
+from tests.attn_util import bf16, check, f32_1, i32, offsets, paged, same
+from tests.gpu_util import announce, need_gpu, u16
+
+pytestmark = pytest.mark.gpu
+KS, VS, SM = np.float32(0.02), np.float32(0.03), 0.02
+
+
+@pytest.fixture(scope="module")
+def fp8rl():
+    need_gpu()
+    import paper_2601_18150_amd as m
+    m.load()
+    return m
+
+
+def chunk_args(kc, vc, table, lens, cu, max_len):
+    return [torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda(), i32(table), i32(lens), i32(cu), max_len, f32_1(KS),
+            f32_1(VS), SM]
+
+
+# rows of a run: 32 a small tile, up to 64 in small tiles, 128 a large one
+@pytest.mark.parametrize("heads,new", [(1, 31), (1, 32), (1, 33), (1, 64), (1, 65), (1, 128), (1, 129), (4, 8), (4, 9), (4, 16),
+                                       (4, 17), (8, 8), (8, 9), (8, 33)])
+def test_rows_at_the_edges_of_tiles(fp8rl, heads, new):
+    announce(f"chunk: {heads} heads over one, {new} new tokens")
+    rng = np.random.default_rng(heads * 1000 + new)
+    lens, news = [new + 150, new, 77], [new, new, 1]
+    kc, vc, table = paged(rng, lens, 1)
+    cu = offsets(news)
+    q = bf16(rng, (sum(news), heads, 128))
+    out = fp8rl.fp8rl_attention_prompt_fp8kv(q.cuda(), *chunk_args(kc, vc, table, lens, cu, max(lens)))
+    torch.cuda.synchronize()
+    check(out, attention.prompt_paged(u16(q), kc, vc, KS, VS, table, lens, cu, SM), max(lens), attention.FP8_VALUES, "chunk")
+
+
+# shares of a sequence's own pages that are no whole number of 32-key chunks, and the last one partly filled
+@pytest.mark.parametrize("own", [1, 31, 255, 256, 257, 500, 528, 545, 815, 1100, 2049])
+def test_shares_of_pages(fp8rl, own):
+    announce(f"shared: {own} own tokens behind a prefix of 48")
+    rng = np.random.default_rng(own)
+    lens = [48 + own, 48 + max(1, own // 3)]
+    kc, vc, table = paged(rng, lens, 1)
+    table[1, :3] = table[0, :3]
+    q = bf16(rng, (2, 4, 128))
+    out = fp8rl.fp8rl_attention_decode_shared_fp8kv(
+        q.cuda(), torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda(), i32(table), i32(lens), i32([0, 2]), i32([48]), 48,
+        max(lens), f32_1(KS), f32_1(VS), SM)
+    torch.cuda.synchronize()
+    check(out, attention.prompt_paged(u16(q), kc, vc, KS, VS, table, lens, [0, 1, 2], SM), max(lens), attention.FP8_VALUES,
+          "shared")
+
+
+def test_caches_past_4_gib(fp8rl):
+    """Blocks spread over 4.6 GB of keys and of values: offsets of pages, chunks and copies past 32 bits."""
+    announce("caches of 280000 blocks x 8 kv heads")
+    rng = np.random.default_rng(1)
+    lens = [300, 90, 1000]
+    kc, vc, table = paged(rng, lens, 8)
+    blocks = 280000
+    at = np.sort(rng.choice(np.arange(200000, blocks), len(kc), replace=False))
+    at[0], at[-1] = 0, blocks - 1
+    ids = torch.from_numpy(at).cuda()
+    big_k = torch.zeros((blocks, 8, 16, 128), dtype=torch.uint8, device="cuda")
+    big_v = torch.zeros((blocks, 8, 4, 128, 4), dtype=torch.uint8, device="cuda")
+    big_k[ids], big_v[ids] = torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda()
+    used = np.arange(table.shape[1])[None] < (np.array(lens)[:, None] + 15) // 16
+    far = np.where(used, at[np.clip(table, 0, len(at) - 1)], -1).astype(np.int32)
+    new = [40, 3, 1]                                     # large tiles, small ones
+    cu = offsets(new)
+    q = bf16(rng, (44, 16, 128))
+    out = fp8rl.fp8rl_attention_prompt_fp8kv(q.cuda(), big_k, big_v, i32(far), i32(lens), i32(cu), 1000, f32_1(KS), f32_1(VS), SM)
+    torch.cuda.synchronize()
+    check(out, attention.prompt_paged(u16(q), kc, vc, KS, VS, table, lens, cu, SM), 1000, attention.FP8_VALUES, "chunk")
+    q = bf16(rng, (3, 16, 128))
+    out = fp8rl.fp8rl_attention_decode_shared_fp8kv(q.cuda(), big_k, big_v, i32(far), i32(lens), i32([0, 2, 3]), i32([80, 512]),
+                                                    512, 1000, f32_1(KS), f32_1(VS), SM)
+    torch.cuda.synchronize()
+    seen = attention.shared_table(table, lens, [0, 2, 3], [80, 512], 512)
+    check(out, attention.prompt_paged(u16(q), kc, vc, KS, VS, seen, lens, np.arange(4), SM), 1000, attention.FP8_VALUES, "shared")
+    announce("copy and compact of the same")
+    fp8rl.fp8rl_kv_copy_blocks([big_k, big_v], i32([at[-1]]), i32([blocks - 3]))
+    torch.cuda.synchronize()
+    assert torch.equal(big_k[blocks - 3], big_k[blocks - 1]) and torch.equal(big_v[blocks - 3], big_v[blocks - 1])
+    refs = torch.zeros(blocks, dtype=torch.int32, device="cuda")
+    refs[torch.from_numpy(far[used]).cuda().long()] = 1
+    state = [i32(far), i32(lens), refs]
+    live = fp8rl.fp8rl_kv_compact([big_k, big_v], *state)
+    torch.cuda.synchronize()
+    assert int(live) == used.sum() and torch.all(refs[:int(live)] == 1) and int(refs.sum()) == int(live)
+    now = state[0].cpu().numpy()
+    assert np.array_equal(big_k[torch.from_numpy(now[used]).cuda().long()].cpu().numpy(), kc[table[used]])
+    assert np.array_equal(big_v[torch.from_numpy(now[used]).cuda().long()].cpu().numpy(), vc[table[used]])
+
+
+def test_on_a_stream_of_its_own_and_two_at_once(fp8rl):
+    """Inputs made on one stream, calls on two others without anything to order them but the events: each allocates its
+    own workspace and output there."""
+    announce("chunk and shared on side streams")
+    rng = np.random.default_rng(2)
+    lens, new = [3000, 700], [2, 40]
+    kc, vc, table = paged(rng, lens, 2)
+    cu = offsets(new)
+    qs = [bf16(rng, (42, 8, 128)).cuda() for _ in range(6)]
+    args = chunk_args(kc, vc, table, lens, cu, 3000)
+    group = [i32([0, 2]), i32([640]), 640, 3000]
+
+    def both(q, stream=None):
+        a = fp8rl.fp8rl_attention_prompt_fp8kv(q, *args, stream=stream)
+        b = fp8rl.fp8rl_attention_decode_shared_fp8kv(q[:2], *args[:4], *group, *args[6:], stream=stream)
+        return a, b
+
+    want = [both(q) for q in qs]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [both(q, streams[i % 2]) for i, q in enumerate(qs)]
+    by_handle = both(qs[0], streams[0].cuda_stream)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        same(g[0], w[0], "chunk on a side stream")
+        same(g[1], w[1], "shared on a side stream")
+    same(by_handle[0], want[0][0], "chunk on a stream by its handle")
+    same(by_handle[1], want[0][1], "shared on a stream by its handle")
