@@ -153,34 +153,34 @@ __device__ __forceinline__ void attn_load_q(const AttnRow& row, bf16x8 (&q)[8]) 
     q[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row.q + 16 * kk + 8 * h));
 }
 
-// Where a lane's operands lie in a tile: keys of 16-dim step kk and 32-key half b at k[kk] + 32 b rows,
-// values of dims 32 d and 16-key step t at v[d] + 16 t rows (bf16), v[0] + value16_at(t, 0, 32 d) (f16).
+// Where a lane's operands lie in a tile: keys of 16-dim step kk and 32-key half b, values of dims 32 d and
+// 16-key step t.
 template <bool kF16Values>
 struct LaneOffsets {
-  int k[8];
-  int v[kF16Values ? 1 : 4];
+  int k, v;                // of kk = 0, and of d = 0: the permutations are exclusive ors, so that the others' offsets
+                           // differ in one bit field each, and no register has to hold them
 
   __device__ __forceinline__ LaneOffsets() {
     const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) k[kk] = key_at(j, 2 * kk + h);
-    if constexpr (kF16Values) {
-      v[0] = value16_at(0, h, j);
-    } else {
-      // ds_read_b64_tr_b16: of 16 lanes that point at four rows x 16 columns, lane i gets column i
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-        v[d] = value_at(4 * h + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
-    }
+    k = key_at(j, h);
+    // ds_read_b64_tr_b16: of 16 lanes that point at four rows x 16 columns, lane i gets column i
+    v = kF16Values ? value16_at(0, h, j)
+                   : value_at(4 * h + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
+  }
+  // The offsets as they are needed (and not held across the loop).
+  __device__ __forceinline__ LaneOffsets fresh() const {
+    LaneOffsets f = *this;
+    asm volatile("" : "+v"(f.k), "+v"(f.v));
+    return f;
   }
   __device__ __forceinline__ bf16x8 key(const uint8_t* keys, int i) const {     // i: 8 * half + step
-    return *reinterpret_cast<const bf16x8*>(keys + k[i & 7] + (i >> 3) * 32 * 256);
+    return *reinterpret_cast<const bf16x8*>(keys + (k ^ ((i & 7) << 5)) + (i >> 3) * 32 * 256);
   }
   __device__ __forceinline__ uint4 value(const uint8_t* values, int i) const {  // i: 4 * step + d
     if constexpr (kF16Values) {
-      return *reinterpret_cast<const uint4*>(values + v[0] + value16_at(i >> 2, 0, 32 * (i & 3)));
+      return *reinterpret_cast<const uint4*>(values + v + value16_at(i >> 2, 0, 32 * (i & 3)));
     } else {
-      const uint8_t* at = values + v[i & 3] + (i >> 2) * 16 * 256;
+      const uint8_t* at = values + (v ^ ((i & 3) << 6)) + (i >> 2) * 16 * 256;
       const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at)));
       const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * 256)));
       return make_uint4(lo.x, lo.y, hi.x, hi.y);
@@ -259,7 +259,8 @@ __device__ __forceinline__ void scale_if(uint64_t any, f32x16 (&o)[4], float alp
 // relative, against bf16 ones 2^-9, of the size of the output's own rounding.
 template <bool kF16Values, bool kMask>
 __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int k0, float c,
-                                            const LaneOffsets<kF16Values>& at, const uint8_t* keys, uint32_t (&p)[16]) {
+                                            const LaneOffsets<kF16Values>& lane_at, const uint8_t* keys, uint32_t (&p)[16]) {
+  const LaneOffsets<kF16Values> at = lane_at.fresh();
   const int h = (threadIdx.x & 63) >> 5;
   f32x16 s[2] = {(f32x16)(0.0f), (f32x16)(0.0f)};
 #pragma unroll
@@ -304,8 +305,9 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
 
 // O^T += V^T P^T over the tile's values in LDS.
 template <bool kF16Values>
-__device__ __forceinline__ void attn_values(AttnAcc& acc, const uint32_t (&p)[16], const LaneOffsets<kF16Values>& at,
+__device__ __forceinline__ void attn_values(AttnAcc& acc, const uint32_t (&p)[16], const LaneOffsets<kF16Values>& lane_at,
                                             const uint8_t* values) {
+  const LaneOffsets<kF16Values> at = lane_at.fresh();
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int t = i >> 2;
@@ -455,7 +457,7 @@ __device__ __forceinline__ void store_values(Fp8Values f, int k0, int len, uint8
   }
 }
 
-// All tiles of keys begin .. end - 1.  LDS holds one tile of keys and one of values, each refilled while
+// All tiles of keys begin .. end - 1 (one at least).  LDS holds one tile of keys and one of values, each refilled while
 // the other is in use: the values land under the score product, the next keys under the softmax and the
 // value product.  Two barriers a tile: behind the first (next_values) every wave has read the values
 // before and the keys are there, behind the second (next_keys) every wave has read the keys and the
@@ -495,16 +497,21 @@ __device__ __forceinline__ void attn_run(AttnAcc& acc, const bf16x8 (&q)[8], con
 __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
                                               float c, const Bf16Rows<false>& k, const Bf16Rows<true>& v,
                                               const TileLds& lds) {
-  if (begin >= end) return;
   k.load(begin, lds.k);
+  v.load(begin, lds.v);                                    // (the first tile's come with its keys)
   attn_run<false>(acc, q, row, begin, end, c, lds, [&](int k0) {
     wait_vmcnt<0>();
     lds_barrier();
     if (k0 < end) k.load(k0, lds.k);
   }, [&](int k0) {
-    wait_vmcnt<0>();
-    lds_barrier();
-    v.load(k0, lds.v);
+    if (k0 == begin) {
+      wait_vmcnt<kTileLoads>();
+      lds_barrier();
+    } else {
+      wait_vmcnt<0>();
+      lds_barrier();
+      v.load(k0, lds.v);
+    }
   });
 }
 
@@ -515,7 +522,6 @@ __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8]
 // contexts and a tenth longer over short ones.)
 __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
                                              float c, const PagedKv& pages, int len, const TileLds& lds) {
-  if (begin >= end) return;
   Fp8Keys fk;
   Fp8Values fv;
   Fp8Pages at = tile_pages(pages, begin, len), after = tile_pages(pages, begin + kTileKeys, len);

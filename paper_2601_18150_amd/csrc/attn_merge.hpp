@@ -107,7 +107,7 @@ __device__ __forceinline__ void merge_few_records(const float* __restrict__ base
 }
 
 // Records up to which 32 lanes join them alone.
-constexpr int kFewRecords = 8;
+constexpr int kFewRecords = 16;
 
 }  // namespace
 }  // namespace fp8rl

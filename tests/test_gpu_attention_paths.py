@@ -25,9 +25,9 @@ def chunk_args(kc, vc, table, lens, cu, max_len):
             f32_1(VS), SM]
 
 
-# rows of a run: 32 a small tile, up to 64 in small tiles, 128 a large one
-@pytest.mark.parametrize("heads,new", [(1, 31), (1, 32), (1, 33), (1, 64), (1, 65), (1, 128), (1, 129), (4, 8), (4, 9), (4, 16),
-                                       (4, 17), (8, 8), (8, 9), (8, 33)])
+# rows of a run: 32 a small tile, up to 96 in small tiles, 128 a large one
+@pytest.mark.parametrize("heads,new", [(1, 31), (1, 32), (1, 33), (1, 64), (1, 65), (1, 96), (1, 97), (1, 128), (1, 129), (4, 8), (4, 9), (4, 16),
+                                       (4, 17), (8, 8), (8, 9), (8, 12), (8, 13), (8, 33)])
 def test_rows_at_the_edges_of_tiles(fp8rl, heads, new):
     announce(f"chunk: {heads} heads over one, {new} new tokens")
     rng = np.random.default_rng(heads * 1000 + new)
