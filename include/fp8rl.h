@@ -459,7 +459,9 @@ int fp8rl_attention_decode_bf16kv(const uint16_t* q, const uint16_t* k_cache, co
  *      total (precondition; offsets are clamped into [0, total], so that nothing outside the rows is
  *      touched).  Sequences may be empty; rows before the first offset or from the last one on are
  *      read by no sequence and written by none.
- * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; total * q_heads / 128 + 2 * batch * kv_heads < 2^23
+ * What a row does not attend to does not reach it, NaN and infinities among later tokens' values
+ * included; a row whose scores are all -inf gives NaN.
+ * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; total * q_heads / 128 + 3 * batch * kv_heads < 2^23
  * (else FP8RL_ERR_UNSUPPORTED_SHAPE).  total == 0 or batch == 0 is a no-op.
  * Alignment: q, k, v, out 16-byte, every ld a multiple of 8, cu_seqlens 4-byte.
  */

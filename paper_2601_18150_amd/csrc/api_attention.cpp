@@ -154,9 +154,9 @@ int fp8rl_attention_decode_shared_fp8kv(const uint16_t* q, const uint8_t* k_cach
       num_blocks >= kMaxDim)
     return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (batch == 0) return FP8RL_OK;
-  if (batch * q_heads >= kMaxGrid ||
+  if (batch * q_heads >= kMaxGrid / 2 ||
       fp8rl::attn_shared_workgroups(batch, num_groups, q_heads / kv_heads, kv_heads, max_prefix_len, max_seq_len) >=
-          kMaxGrid)
+          2 * kMaxGrid)                             // (a workgroup for each sequence and kv head, and for each prefix)
     return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (!q || !out || !group_offsets || !prefix_lens || !workspace) return FP8RL_ERR_INVALID_ARG;
   st = check_paged(k_cache, v_cache, num_blocks, block_table, max_blocks, seq_lens, max_seq_len, k_scale, v_scale);

@@ -113,7 +113,6 @@ struct AttnRow {
   const uint16_t* q;       // its 128 query values
   int limit;               // last key it attends to (below the first key: none)
   int all_limit;           // the smallest limit of the workgroup's rows (no mask is needed up to it)
-  int wave_last;           // the largest of the wave's (tiles behind it are skipped)
 };
 
 // Running state of a wave: lane L holds dims 8 (i / 4) + 4 (L / 32) + i % 4 of each 32 of row L % 32.
@@ -541,6 +540,94 @@ __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8],
     store_values(fv, k0, len, lds.v);
     fetch_values(pages, at, fv);
   });
+}
+
+// Single keys and values as the lanes of attn_redo take them: the half's part of q . k (dims 16 kk + 8 h ..), and
+// the values of four dims.
+struct Bf16Tokens {
+  const uint16_t* k;
+  int64_t ld_k;
+  const uint16_t* v;
+  int64_t ld_v;
+
+  __device__ __forceinline__ float score(const bf16x8 (&q)[8], int t, int h) const {
+    float s = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const bf16x8 x = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k + t * ld_k + 16 * kk + 8 * h));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf((float)x[i], (float)q[kk][i], s);
+    }
+    return s;
+  }
+  __device__ __forceinline__ float4 values(int t, int dim) const {
+    const uint2 x = *reinterpret_cast<const uint2*>(v + t * ld_v + dim);
+    return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
+                       __uint_as_float(x.y & 0xFFFF0000u));
+  }
+};
+
+struct Fp8Tokens {
+  const PagedKv& c;
+
+  __device__ __forceinline__ float score(const bf16x8 (&q)[8], int t, int h) const {
+    const uint8_t* at = c.k + page_offset(c, page_entry(c, t / kPageTokens)) + t % kPageTokens * kHeadDim + 8 * h;
+    float s = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const uint2 w = *reinterpret_cast<const uint2*>(at + 16 * kk), a = bf16_of_fp8(w.x), b = bf16_of_fp8(w.y);
+      const bf16x8 x = __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf((float)x[i], (float)q[kk][i], s);
+    }
+    return s;
+  }
+  __device__ __forceinline__ float4 values(int t, int dim) const {   // (a dword holds four tokens of a dim)
+    const uint4 w = *reinterpret_cast<const uint4*>(c.v + page_offset(c, page_entry(c, t / kPageTokens)) +
+                                                    (t % kPageTokens / 4 * kHeadDim + dim) * 4);
+    const int b = 8 * (t % 4);
+    return make_float4(__builtin_amdgcn_cvt_f32_fp8((int)(w.x >> b), 0), __builtin_amdgcn_cvt_f32_fp8((int)(w.y >> b), 0),
+                       __builtin_amdgcn_cvt_f32_fp8((int)(w.z >> b), 0), __builtin_amdgcn_cvt_f32_fp8((int)(w.w >> b), 0));
+  }
+};
+
+// In a tile of which some rows see less, a value that is not finite would make their sums NaN too (0 x NaN in the
+// product).  Rows whose sums are not finite are summed anew here, over the keys that they see alone and in the
+// order of the keys: runs of `run` keys, `step` apart.  Slow, and only for such values; a row that sees one gets the same
+// again.  Everything else pays a sum of 64 products with zero for each lane at the end.
+template <class Tokens>
+__device__ __forceinline__ void attn_redo(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end, int run,
+                                          int step, float c, const Tokens& tokens) {
+  float z = 0.0f;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z = fmaf(acc.o[d][i], 0.0f, z);
+  const uint64_t bad = __ballot(z != 0.0f);
+  if (bad == 0) return;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const bool mine = ((bad | bad >> 32) >> (lane & 31)) & 1;
+  const float mc = fmaxf(acc.m * c, kNoScore);
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc.o[d][i] = mine ? 0.0f : acc.o[d][i];
+  for (int k0 = begin; k0 < end; k0 += step)
+    for (int t = k0; t < min(k0 + run, end); ++t) {
+      const float s = half_sum(tokens.score(q, t, h));
+      const bool sees = mine && t <= row.limit;
+      const float e = __builtin_amdgcn_exp2f(fmaf(s, c, -mc));
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 v = tokens.values(t, 32 * d + 8 * g + 4 * h);
+          acc.o[d][4 * g] = sees ? fmaf(e, v.x, acc.o[d][4 * g]) : acc.o[d][4 * g];
+          acc.o[d][4 * g + 1] = sees ? fmaf(e, v.y, acc.o[d][4 * g + 1]) : acc.o[d][4 * g + 1];
+          acc.o[d][4 * g + 2] = sees ? fmaf(e, v.z, acc.o[d][4 * g + 2]) : acc.o[d][4 * g + 2];
+          acc.o[d][4 * g + 3] = sees ? fmaf(e, v.w, acc.o[d][4 * g + 3]) : acc.o[d][4 * g + 3];
+        }
+    }
 }
 
 // Dims 32 d + 8 g + 4 h .. + 3 of this lane's row, of the eight that the half's pair of lanes share:

@@ -132,6 +132,8 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
       }
     }
   }
+  if (__ballot(row.limit < end - 1))
+    attn_redo(acc, q, row, begin + wave * kChunkKeys, end, kChunkKeys, kAttnWaves * kChunkKeys, c, Fp8Tokens{pages});
   acc.l = half_sum(acc.l);
 }
 

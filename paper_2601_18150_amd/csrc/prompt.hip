@@ -74,7 +74,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   AttnRow row;
   row.q = p.q + token * p.ld_q + head * kHeadDim;
   row.limit = position(r);
-  row.wave_last = position(row0 + kRowsPerWave * wave + kRowsPerWave - 1);
   const int split = blockIdx.y;
   const int begin = kFp8 ? split * p.split_keys : 0;
   const int end = min(position(row0 + tile - 1) + 1, kFp8 && p.splits > 1 ? begin + p.split_keys : 0x7FFFFFFF);
@@ -119,7 +118,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
           rec[group * kHeadDim + group + hd] = l;
         }
       } else {
-        store16_bf16(o, l == 0.0f ? 0.0f : p.v_scale[0] / l, p.out + tok * p.ld_out + (kvh * group + hd) * kHeadDim + 16 * part);
+        store16_bf16(o, position(ri) < 0 ? 0.0f : p.v_scale[0] / l, p.out + tok * p.ld_out + (kvh * group + hd) * kHeadDim + 16 * part);
       }
     });
     return;
@@ -130,15 +129,17 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   attn_load_q(row, q);
   if constexpr (kFp8) {
     attn_run_fp8(acc, q, row, begin, end, c, pages, len, lds);
+    if (row.all_limit < end - 1) attn_redo(acc, q, row, begin, end, end, end, c, Fp8Tokens{pages});
   } else {
     const Bf16Rows<false> k(static_cast<const uint16_t*>(p.k) + at.first * p.ld_k + kvh * kHeadDim, p.ld_k, len);
     const Bf16Rows<true> v(static_cast<const uint16_t*>(p.v) + at.first * p.ld_v + kvh * kHeadDim, p.ld_v, len);
     attn_run_bf16(acc, q, row, begin, end, c, k, v, lds);
+    if (row.all_limit < end - 1) attn_redo(acc, q, row, begin, end, end, end, c, Bf16Tokens{k.base, k.ld, v.base, v.ld});
   }
   const float l = half_sum(acc.l);
   const bool valid = r < rows;
   if (direct) {
-    const float f = l == 0.0f ? 0.0f : (kFp8 ? p.v_scale[0] : 1.0f) / l;   // no visible key: 0
+    const float f = position(r) < 0 ? 0.0f : (kFp8 ? p.v_scale[0] : 1.0f) / l;   // no visible key: 0
     attn_store_bf16(acc, f, p.out + token * p.ld_out + head * kHeadDim, valid);
     return;
   }

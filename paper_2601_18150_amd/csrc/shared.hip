@@ -175,6 +175,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_shared_kernel(const S
   bf16x8 q[8];
   attn_load_q(row, q);
   attn_run_fp8(acc, q, row, begin, end, c, pages, prefix, lds);
+  if (row.all_limit < end - 1) attn_redo(acc, q, row, begin, end, end, end, c, Fp8Tokens{pages});
   const float l = half_sum(acc.l);
   const bool valid = r < rows;
   const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;

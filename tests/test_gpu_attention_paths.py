@@ -128,3 +128,99 @@ def test_on_a_stream_of_its_own_and_two_at_once(fp8rl):
         same(g[1], w[1], "shared on a side stream")
     same(by_handle[0], want[0][0], "chunk on a stream by its handle")
     same(by_handle[1], want[0][1], "shared on a stream by its handle")
+
+
+def finite_alone(got, res, clean, keys, kind, what):
+    """Where the oracle is finite the outputs are within the bound of the same inputs without the values that are not
+    (`clean`: a row that sees them has other dims of which they are no part); elsewhere they are the oracle's."""
+    g = got.float().cpu().numpy().astype(np.float64).reshape(res[0].shape)
+    ok = np.isfinite(res[0])
+    assert not ok.all() and ok.any()
+    assert np.array_equal(g[~ok], res[0][~ok], equal_nan=True), f"{what}: not the oracle's where it is not finite"
+    check(torch.from_numpy(np.where(ok, g, np.nan)), (np.where(ok, clean[0], np.nan), *clean[1:]), keys, kind, what)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (4, 2)])
+@pytest.mark.parametrize("at", [0, 40, 100, 149])
+def test_values_that_are_not_finite_reach_later_prompt_rows_alone(fp8rl, heads, kv_heads, at):
+    announce(f"prompt: {heads}/{kv_heads} heads, NaN and inf among the values of token {at}, a NaN key behind it")
+    rng = np.random.default_rng(heads + at)
+    n = 200
+    cu = [0, n, n + 30]
+    q, k, v = bf16(rng, (n + 30, heads, 128)), bf16(rng, (n + 30, kv_heads, 128)), bf16(rng, (n + 30, kv_heads, 128))
+    clean = attention.prompt(u16(q), u16(k), u16(v), cu, 0.09)
+    v[at, 0, 5], v[at, kv_heads - 1, 77], v[at + 1, 0, 9], k[at + 30, 0, 3] = float("nan"), float("inf"), -float("inf"), float("nan")
+    with np.errstate(invalid="ignore"):
+        res = attention.prompt(u16(q), u16(k), u16(v), cu, 0.09)
+    out = fp8rl.fp8rl_attention_prompt_bf16(q.cuda(), k.cuda(), v.cuda(), i32(cu), 0.09)
+    torch.cuda.synchronize()
+    finite_alone(out, res, clean, n, attention.BF16_VALUES, "prompt")
+
+
+def poison(vc, table, b, token, dim):
+    vc[table[b, token // 16], :, token % 16 // 4, dim, token % 4] = 0x7F
+
+
+# small tiles and large ones, whole and in records
+@pytest.mark.parametrize("heads,kv_heads,lens,new", [(2, 1, [150, 40], [20, 5]), (8, 1, [150, 170], [40, 3]),
+                                                     (4, 1, [3000, 700], [6, 20]), (8, 2, [1500, 2100], [33, 70])])
+def test_nan_codes_of_later_tokens_do_not_reach_a_chunk(fp8rl, heads, kv_heads, lens, new):
+    announce(f"chunk: {heads}/{kv_heads} heads, lengths {lens}, new {new}, NaN codes among the new tokens' values")
+    rng = np.random.default_rng(heads + new[0])
+    kc, vc, table = paged(rng, lens, kv_heads)
+    cu = offsets(new)
+    q = bf16(rng, (sum(new), heads, 128))
+    args = [u16(q), kc, vc, KS, VS, table, lens, cu, SM]
+    clean = attention.prompt_paged(*args)
+    for b, (n, m) in enumerate(zip(lens, new)):
+        poison(vc, table, b, n - 1, 3)
+        poison(vc, table, b, n - m // 2, 100)
+    res = attention.prompt_paged(*args)
+    out = fp8rl.fp8rl_attention_prompt_fp8kv(q.cuda(), *chunk_args(kc, vc, table, lens, cu, max(lens)))
+    torch.cuda.synchronize()
+    finite_alone(out, res, clean, max(lens), attention.FP8_VALUES, "chunk")
+
+
+@pytest.mark.parametrize("heads,members", [(2, 5), (8, 40)])
+def test_nan_codes_behind_a_short_member_do_not_reach_it(fp8rl, heads, members):
+    """Members shorter than their prefix: what the others read behind their end is not theirs."""
+    announce(f"shared: {members} members of {heads} heads, NaN codes in the prefix behind the short ones")
+    rng = np.random.default_rng(members)
+    lens = [900] + [int(x) for x in rng.integers(1, 900, members - 1)]
+    kc, vc, table = paged(rng, [900] * members, 1)
+    table[1:] = table[0]
+    q = bf16(rng, (members, heads, 128))
+    args = [u16(q), kc, vc, KS, VS, table, lens, np.arange(members + 1), SM]
+    clean = attention.prompt_paged(*args)
+    for t in (100, 333, 640, 890):
+        poison(vc, table, 0, t, t % 128)
+    res = attention.prompt_paged(*args)
+    out = fp8rl.fp8rl_attention_decode_shared_fp8kv(
+        q.cuda(), torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda(), i32(table), i32(lens), i32([0, members]), i32([896]),
+        896, 900, f32_1(KS), f32_1(VS), SM)
+    torch.cuda.synchronize()
+    finite_alone(out, res, clean, 900, attention.FP8_VALUES, "shared")
+
+
+@pytest.mark.parametrize("new,length", [(3, 3), (40, 200), (2, 3000)])
+def test_a_row_whose_scores_are_all_minus_infinity(fp8rl, new, length):
+    """No softmax exists of them: NaN, whichever way the row takes; the rows beside it keep theirs."""
+    announce(f"chunk and prompt: {new} of {length} tokens, one row of -inf scores")
+    rng = np.random.default_rng(new)
+    kc, vc, table = paged(rng, [length], 1)
+    kc[:, :, :, 0] = 0x7E                                # 448 in dim 0 of every key
+    q = bf16(rng, (new, 4, 128))
+    q[:, :, 0] = 0.0
+    res = attention.prompt_paged(u16(q), kc, vc, KS, VS, table, [length], [0, new], SM)
+    q[1, 2, 0] = -3e38
+    out = fp8rl.fp8rl_attention_prompt_fp8kv(q.cuda(), *chunk_args(kc, vc, table, [length], [0, new], length))
+    k, v = torch.zeros((new, 1, 128), dtype=torch.bfloat16), bf16(rng, (new, 1, 128))
+    k[:, :, 0] = 448.0
+    prompt = fp8rl.fp8rl_attention_prompt_bf16(q.cuda(), k.cuda(), v.cuda(), i32([0, new]), SM)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[1, 2]).all() and torch.isnan(prompt[1, 2]).all()
+    out, prompt = out.clone(), prompt.clone()
+    out[1, 2] = torch.from_numpy(res[0][1, 2]).to(out)
+    prompt[1, 2] = 0.0
+    check(out, res, length, attention.FP8_VALUES, "chunk")
+    assert torch.isfinite(prompt).all()
