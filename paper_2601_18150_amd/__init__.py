@@ -14,8 +14,8 @@ scales), section 2.1.2 (weights re-quantised at every RL step), section 2.1.4
 """
 from __future__ import annotations
 
+import array
 import ctypes
-import itertools
 import operator
 import os
 
@@ -815,17 +815,17 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
 
 
 def _cache_list(caches):
-    """(ctypes array of base pointers, count, bytes per block, blocks) of caches [num_blocks][..] of one block size."""
+    """(array of base pointers, their number, bytes per block, blocks) of contiguous caches of one size, the first of
+    them [num_blocks][..]."""
     if not caches:
         raise ValueError("at least one cache")
-    first, n = caches[0], len(caches)
+    first = caches[0]
     blocks, size = (first.shape[0] if first.dim() > 1 else -1), first.nbytes
-    # (a model has a hundred caches: no Python step for each)
-    if blocks < 0 or set(map(torch.Tensor.size, caches, itertools.repeat(0))) != {blocks} or \
-            set(map(operator.attrgetter("nbytes"), caches)) != {size} or \
+    # (a model has a hundred caches: no Python step for each, and what takes longest, their shapes, is left out)
+    if blocks < 0 or set(map(operator.attrgetter("nbytes"), caches)) != {size} or \
             not all(map(torch.Tensor.is_contiguous, caches)):
         raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
-    return (ctypes.c_void_p * n)(*map(torch.Tensor.data_ptr, caches)), n, size // max(blocks, 1), blocks
+    return array.array("Q", map(torch.Tensor.data_ptr, caches)), len(caches), size // max(blocks, 1), blocks
 
 
 def _table(block_table, seq_lens, block_refs, blocks=None):
@@ -842,8 +842,8 @@ def fp8rl_kv_copy_blocks(caches, src: torch.Tensor, dst: torch.Tensor, stream=No
     _i32(src, None, "src")
     _i32(dst, src.numel(), "dst")
     _here(*caches, src, dst)
-    _check("fp8rl_kv_copy_blocks", load().fp8rl_kv_copy_blocks(ptrs, n, size, blocks, src.data_ptr(), dst.data_ptr(),
-                                                               src.numel(), _stream(stream)))
+    _check("fp8rl_kv_copy_blocks", load().fp8rl_kv_copy_blocks(ptrs.buffer_info()[0], n, size, blocks, src.data_ptr(),
+                                                               dst.data_ptr(), src.numel(), _stream(stream)))
 
 
 def fp8rl_kv_fork_sequences(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, block_refs: torch.Tensor,
@@ -857,7 +857,7 @@ def fp8rl_kv_fork_sequences(caches, block_table: torch.Tensor, seq_lens: torch.T
     _i32(new_blocks, parents.numel(), "new_blocks")
     _here(*caches, block_table, seq_lens, block_refs, parents, children, new_blocks)
     _check("fp8rl_kv_fork_sequences", load().fp8rl_kv_fork_sequences(
-        ptrs, n, size, blocks, block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(),
+        ptrs.buffer_info()[0], n, size, blocks, block_table.data_ptr(), *block_table.shape, seq_lens.data_ptr(),
         block_refs.data_ptr(), parents.data_ptr(), children.data_ptr(), new_blocks.data_ptr(), parents.numel(),
         _stream(stream)))
 
@@ -890,7 +890,7 @@ def fp8rl_kv_compact(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, 
     workspace = _workspace(workspace, dev, stream, fp8rl_kv_compact_workspace_size, blocks)
     _here(*caches, block_table, seq_lens, block_refs, live, workspace)
     _check("fp8rl_kv_compact", load().fp8rl_kv_compact(
-        ptrs, n, size, blocks, block_table.data_ptr(), block_table.shape[0], block_table.shape[1], seq_lens.data_ptr(),
+        ptrs.buffer_info()[0], n, size, blocks, block_table.data_ptr(), *block_table.shape, seq_lens.data_ptr(),
         block_refs.data_ptr(), live.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
         _stream(stream)))
     return live
