@@ -177,11 +177,16 @@ int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int6
   return attn_tile_bound(total * group, batch < total ? batch : total, fp8 ? kPromptSmall : 0) * kv_heads;
 }
 
-// Splits of the keys where the tiles alone are too few for the 512 workgroups that the chip holds:
-// as many as fill them, of at least 256 keys each.
+// Splits of the keys where the tiles alone are too few for the 512 workgroups that the chip holds: as many as
+// fill them, of at least 256 keys each.  Over long sequences half as many again, so that no second round
+// of a few whole tiles follows the first (512 / 768 workgroups, us: one chunk of 1225 behind 12574 tokens 391 /
+// 318, two of up to 1802 behind 13830 738 / 652; four of up to 1277 behind 870 82 / 92, two of 1013 behind 261 44 / 50:
+// there the records cost more than the round; few drafted tokens, small tiles, behind 11388 tokens 40 / 46).
 PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len) {
-  const int64_t wgs = attn_tile_guess(total * group, batch < total ? batch : total, kPromptSmall) * kv_heads;
-  int64_t splits = wgs > 0 ? (512 + wgs - 1) / wgs : 1;
+  const int64_t runs = batch < total ? batch : total;
+  const int64_t wgs = attn_tile_guess(total * group, runs, kPromptSmall) * kv_heads;
+  const int64_t target = max_seq_len >= 4096 && total * group > runs * kPromptSmall ? 768 : 512;
+  int64_t splits = wgs > 0 ? (target + wgs - 1) / wgs : 1;
   int64_t keys = (max_seq_len + splits - 1) / splits;
   keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;
   if (keys < 256) keys = 256;
