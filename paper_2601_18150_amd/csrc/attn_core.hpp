@@ -367,12 +367,6 @@ __device__ __forceinline__ uint2 bf16_of_fp8(uint32_t w) {
   return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
 }
 
-// This wave's LDS reads have ended.
-__device__ __forceinline__ void wait_lds() {
-  __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));
-  asm volatile("" ::: "memory");
-}
-
 struct PagedKv {
   const uint8_t* k;
   const uint8_t* v;

@@ -38,6 +38,37 @@ __device__ __forceinline__ void stream_fetch(const PagedKv& c, const int (&blk)[
   }
 }
 
+__device__ __forceinline__ uint32_t lds_offset(const uint8_t* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p;
+}
+
+// A lane's keys and values of a chunk, and the wait for them.  As assembly, because the compiler takes the slot that
+// is read for the one that a chunk is on its way into, and would wait for that one too (with the queries' wait in the
+// loop as well, attn_stream: 16 x 16 sequences of up to 2500 own tokens 176 us, 164 so).
+__device__ __forceinline__ void stream_read(const uint8_t* ks, const int (&key_off)[8], const uint8_t* vs, uint2 (&kf)[8],
+                                            uint2 (&vf)[2][2][2]) {
+  const uint32_t k = lds_offset(ks), v = lds_offset(vs);
+  uint64_t a[8], w[8];
+  asm volatile(
+      "ds_read_b64 %0, %16\n\tds_read_b64 %1, %17\n\tds_read_b64 %2, %18\n\tds_read_b64 %3, %19\n\t"
+      "ds_read_b64 %4, %20\n\tds_read_b64 %5, %21\n\tds_read_b64 %6, %22\n\tds_read_b64 %7, %23\n\t"
+      "ds_read2_b32 %8, %24 offset0:0 offset1:32\n\tds_read2_b32 %9, %25 offset0:0 offset1:32\n\t"
+      "ds_read2_b32 %10, %24 offset0:64 offset1:96\n\tds_read2_b32 %11, %25 offset0:64 offset1:96\n\t"
+      "ds_read2_b32 %12, %26 offset0:0 offset1:32\n\tds_read2_b32 %13, %27 offset0:0 offset1:32\n\t"
+      "ds_read2_b32 %14, %26 offset0:64 offset1:96\n\tds_read2_b32 %15, %27 offset0:64 offset1:96\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(a[4]), "=&v"(a[5]), "=&v"(a[6]), "=&v"(a[7]), "=&v"(w[0]),
+        "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7])
+      : "v"(k + key_off[0]), "v"(k + key_off[1]), "v"(k + key_off[2]), "v"(k + key_off[3]), "v"(k + key_off[4]),
+        "v"(k + key_off[5]), "v"(k + key_off[6]), "v"(k + key_off[7]), "v"(v), "v"(v + 1024), "v"(v + 2048), "v"(v + 3072)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    kf[i] = __builtin_bit_cast(uint2, a[i]);
+    vf[i >> 2][(i >> 1) & 1][i & 1] = __builtin_bit_cast(uint2, w[i]);
+  }
+}
+
 // Keys begin .. end - 1 (begin a multiple of 16; no row's limit is above end - 1) of the len that the
 // sequence has; afterwards every wave has its part in acc.
 __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
@@ -56,10 +87,13 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
   const int chunks = max(0, (end - begin - wave * kChunkKeys + kAttnWaves * kChunkKeys - 1) / (kAttnWaves * kChunkKeys));
   int next[2];
 #pragma unroll
-  for (int d = 0; d < kStreamDepth; ++d) {
+  for (int d = 0; d < kStreamDepth; ++d) {                 // (a wave with fewer chunks reads the last page, as others do)
     entries(d, next);
-    if (d < chunks) stream_fetch(pages, next, keys + d * kChunkBytes, values + d * kChunkBytes);
+    stream_fetch(pages, next, keys + d * kChunkBytes, values + d * kChunkBytes);
   }
+  // The queries were asked for before.  The wait is here, behind a known number of loads that it leaves on their way:
+  // the compiler would put it into the loop, in front of every chunk's products, and there for every load.
+  wait_vmcnt<8 * kStreamDepth>();
   entries(kStreamDepth, next);
   // this lane's operands: keys of row j, 8 dims of half h of 16-byte chunk kk; values of dim j
   int key_off[8];
@@ -73,17 +107,8 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
     uint8_t* ks = keys + slot * kChunkBytes;
     uint8_t* vs = values + slot * kChunkBytes;
     uint2 kf[8];
-    uint32_t vf[2][4][2];                                  // (16-key step, 32 dims, four of the half)
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) kf[kk] = *reinterpret_cast<const uint2*>(ks + key_off[kk]);
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          vf[t][d][u] = *reinterpret_cast<const uint32_t*>(vs + value_off + t * 2048 + d * 128 + u * 1024);
-    wait_lds();                                            // (before the slot is refilled)
+    uint2 vf[2][2][2];                                     // (16-key step, pair of 32 dims, four of the half)
+    stream_read(ks, key_off, vs + value_off, kf, vf);
     if (i + kStreamDepth < chunks) stream_fetch(pages, next, ks, vs);
     entries(i + kStreamDepth + 1, next);
     slot = slot + 1 == kStreamDepth ? 0 : slot + 1;
@@ -114,9 +139,12 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < 2; ++d)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) vf[t][d][u] = keep_bytes(vf[t][d][u], len - (k0 + 16 * t + 8 * u + 4 * h));
+          for (int u = 0; u < 2; ++u) {
+            const int n = len - (k0 + 16 * t + 8 * u + 4 * h);
+            vf[t][d][u] = make_uint2(keep_bytes(vf[t][d][u].x, n), keep_bytes(vf[t][d][u].y, n));
+          }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -127,11 +155,13 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
       const uint4 p = make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7]));
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const uint2 a = f16_of_fp8(vf[t][d][0]), b = f16_of_fp8(vf[t][d][1]);
+        const uint2 x = vf[t][d >> 1][0], y = vf[t][d >> 1][1];
+        const uint2 a = f16_of_fp8(d & 1 ? x.y : x.x), b = f16_of_fp8(d & 1 ? y.y : y.x);
         acc.o[d] = value_mfma<true>(make_uint4(a.x, a.y, b.x, b.y), p, acc.o[d]);
       }
     }
   }
+  wait_vmcnt<0>();
   if (__ballot(row.limit < end - 1))
     attn_redo(acc, q, row, begin + wave * kChunkKeys, end, kChunkKeys, kAttnWaves * kChunkKeys, c, Fp8Tokens{pages});
   acc.l = half_sum(acc.l);

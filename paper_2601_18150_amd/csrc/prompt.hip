@@ -178,14 +178,15 @@ int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int6
 }
 
 // Splits of the keys where the tiles alone are too few for the 512 workgroups that the chip holds: as many as
-// fill them, of at least 256 keys each.  Over long sequences half as many again, so that no second round
-// of a few whole tiles follows the first (512 / 768 workgroups, us: one chunk of 1225 behind 12574 tokens 391 /
-// 318, two of up to 1802 behind 13830 738 / 652; four of up to 1277 behind 870 82 / 92, two of 1013 behind 261 44 / 50:
-// there the records cost more than the round; few drafted tokens, small tiles, behind 11388 tokens 40 / 46).
+// fill them, of at least 256 keys each.  Where that is one or two, over long sequences, half as many again, so
+// that no second round of a few whole tiles follows the first (512 / 768 workgroups, us: one chunk of 1225 behind
+// 12574 tokens 391 / 318, two of up to 1802 behind 13830 738 / 652; shorter sequences, four of up to 1277 behind 870
+// 82 / 92, more splits, 16 chunks of 16 behind 6000 48 / 55, and small tiles, 40 of 4 behind 6000 57 / 63, pay more
+// for the records).
 PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len) {
   const int64_t runs = batch < total ? batch : total;
   const int64_t wgs = attn_tile_guess(total * group, runs, kPromptSmall) * kv_heads;
-  const int64_t target = max_seq_len >= 4096 && total * group > runs * kPromptSmall ? 768 : 512;
+  const int64_t target = max_seq_len >= 4096 && wgs >= 256 && total * group > runs * kPromptSmall ? 768 : 512;
   int64_t splits = wgs > 0 ? (target + wgs - 1) / wgs : 1;
   int64_t keys = (max_seq_len + splits - 1) / splits;
   keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;

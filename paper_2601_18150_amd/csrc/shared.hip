@@ -4,7 +4,10 @@
 // (attn_core.hpp), of 32 where they are few (attn_stream.hpp).  What a member has behind the prefix is
 // read for its own heads alone, by the same stream.  One launch does both, the prefixes' workgroups first:
 // they are bound by arithmetic where groups are large, the others by reading the cache.  A second joins
-// the records (attn_merge.hpp).
+// the records (attn_merge.hpp).  The grid holds every tile that there may be, and every part of a sequence; what has
+// nothing to do lies together at the end of its kind: workgroups go to the XCDs and to the shader engines
+// in turn, and a regular pattern of empty ones left half of those idle (4 prefixes of 18000 tokens, 16 members each: 70
+// us, 50 so).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_shared_kernel(const S
   if (item >= p.prefix_tiles * p.prefix_records) {
     // a sequence's own tokens: record `part` of them, for its own heads
     const int own = item - p.prefix_tiles * p.prefix_records, parts = p.record_count - p.prefix_records;
-    const int b = own / parts, part = own % parts;
+    const int b = own % p.batch, part = own / p.batch;
     const int g = group_of(p, b);
     const int len = clamped_len(p, b);
     const int from = g < 0 ? 0 : shared_prefix(p, g, min(max(p.group_offsets[g], 0), p.batch - 1));
@@ -138,14 +141,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_shared_kernel(const S
     return;
   }
   // a prefix: rows are member r / G of the group, query head r % G of the kv head's
-  const int split = item / p.prefix_tiles;
+  const int split = item % p.prefix_records;
   if (blockIdx.x == 0) {                                // sequences of no group share nothing
     const int lo = p.group_offsets[0], hi = p.group_offsets[p.groups];
     for (int b = threadIdx.x; b < p.batch; b += 64 * kAttnWaves)
       if (b < lo || b >= hi) p.prefix[b] = 0;
   }
   TileOf at;
-  if (!find_tile(p.group_offsets, p.groups, p.batch, p.group_log2, kSharedSmall, item % p.prefix_tiles, at)) return;
+  if (!find_tile(p.group_offsets, p.groups, p.batch, p.group_log2, kSharedSmall, item / p.prefix_records, at)) return;
   at.to_scalars();
   const int rows = at.n << p.group_log2;
   const bool small = rows <= kSharedSmall;
@@ -212,18 +215,17 @@ __global__ __launch_bounds__(kFew ? 256 : 32 * kMergeSets) void attn_shared_merg
 }  // namespace
 
 // Records of a sequence and kv head.  The prefixes' keys are split where their tiles alone are few, 256 keys
-// each at least, so that there are about 256 workgroups of small tiles and 384 of large ones: the chip holds
-// 512, and what is left over goes to the sequences' own tokens, which are bound by reading, meanwhile (us for
-// 256 / 384 / 512: 16 x 16 sequences of 1800 + up to 2500 tokens, small tiles, 176 / 185 / 183; 4 x 32 of 18000
-// + up to 1500, large ones, 98 / 86 / 92).  Own tokens are split where the sequences are fewer than 1024, 256
-// tokens each at least (4 x 8 of 4000 + up to 3000 tokens, for 512 / 1024 / 2048 / 4096: 48 / 47 / 48 / 50 us;
-// 4 x 32 as above 92 / 92 / 94 / 107).
+// each at least, so that there are about 256 workgroups of them: the chip holds 512, and what is left over goes to
+// the sequences' own tokens, which are bound by reading, meanwhile (us for 192 / 256 / 384 / 512: 4 x 32 sequences of
+// 18000 + up to 1500 tokens, large tiles, 93 / 80 / 85 / 91; 2 x 64 of 8000 + 1500 73 / 73 / 80 / 86; small tiles, 16 x
+// 16 of 1800 + 2500, - / 160 / 170 / 170).  Own tokens are split where the sequences are fewer than 1024, 256
+// tokens each at least (8 x 16 of 4000 + up to 800 tokens, for 512 / 1024 / 2048: 51 / 50 / 55; 4 x 32 as above 80 /
+// 80 / 87).
 SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,
                               int64_t max_seq_len) {
   const int64_t runs = groups < batch ? groups : batch;
   const int64_t wgs = attn_tile_guess(batch * group, runs, kSharedSmall) * kv_heads;
-  const int64_t target = batch * group <= runs * kSharedSmall ? 256 : 384;
-  int64_t splits = wgs > 0 ? (target + wgs - 1) / wgs : 1;
+  int64_t splits = wgs > 0 ? (256 + wgs - 1) / wgs : 1;
   int64_t keys = (max_prefix_len + splits - 1) / splits;
   keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;
   if (keys < 256) keys = 256;
