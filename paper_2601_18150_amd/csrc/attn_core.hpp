@@ -211,7 +211,7 @@ constexpr float kMaxGrowth = 8.0f;
 
 // o *= alpha, where any row needs it (any: a bit per lane).  The branches are inside the assembly: as a
 // branch of the program the compiler keeps the accumulators in two places and copies all of them past
-// it in every tile (32 heads over 4, 8191 and 16384 tokens: 2.80 ms; always scaled 2.63; so 2.54).  The products
+// it in every tile (8191 and 16384 tokens, before other steps: 2.80 ms; always scaled 2.63; so 2.54).  The products
 // that made o have ended: alpha comes out of products issued after them.
 __device__ __forceinline__ void scale_if(uint64_t any, f32x16 (&o)[4], float alpha) {
   asm volatile("s_cmp_eq_u64 %14, 0\n\ts_cbranch_scc1 L%=_as_it_is\n\tv_mul_f32 %0, %0, %13\n\tv_mul_f32 %1, %1, %13\n\t"
@@ -456,10 +456,12 @@ __device__ __forceinline__ void store_values(Fp8Values f, int k0, int len, uint8
 // before and the keys are there, behind the second (next_keys) every wave has read the keys and the
 // values are there.  Keys and values are LDS objects of their own, so that the compiler sees that a
 // read of one need not wait for the other's loads.  32 KiB and at most 168 registers leave room for
-// three workgroups on a CU, whose matrix and vector work overlaps (32 heads over 4, 8191 and 16384
-// tokens: 2.63 ms, 1.04 PFLOP/s; two tiles of each in LDS, the score product of the next tile between
-// the instructions of this one's softmax, two workgroups: 2.75 ms, and short prompts took 1.7 times as
-// long; the library's largest bf16 product reaches 1.19 PFLOP/s here, at a clock that falls under load).
+// three workgroups on a CU, whose matrix and vector work overlaps: a wave's tile is 1024 cycles of the one and some
+// 1150 of the other (32 heads over 4, 8191 and 16384 tokens: 2.43 ms, 1.13 PFLOP/s; two tiles of each in LDS, the score
+// product of the next tile between the instructions of this one's softmax, two workgroups: a tenth longer, and
+// short prompts took 1.7 times as long).  The library's largest bf16 product reaches 1.19 PFLOP/s here, at
+// a clock that falls under load: that is what bounds long prompts.  Short ones pay the start and the end of
+// every workgroup (33 of up to 1500 tokens: 0.27 ms, 0.78 PFLOP/s).
 // Tiles that every row sees in full come first and need no mask.
 struct TileLds {
   uint8_t* k;
@@ -512,7 +514,9 @@ __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8]
 // for when those of the one before it have been stored, its page ids a step earlier.  What is asked for
 // behind the last tile repeats the last pages.  (The codes held in registers leave room for two
 // workgroups on a CU; brought through LDS by DMA instead, three of them took as long over long
-// contexts and a tenth longer over short ones.)
+// contexts and a tenth longer over short ones.  Codes asked for two tiles ahead: the same time.)  Three
+// chunks of 2048 against up to 18432 tokens: 1.15 ms, 0.98 PFLOP/s; the widening adds a fifth to the vector work,
+// which a CU with two workgroups overlaps less.
 __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
                                              float c, const PagedKv& pages, int len, const TileLds& lds) {
   Fp8Keys fk;

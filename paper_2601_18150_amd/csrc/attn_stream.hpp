@@ -3,7 +3,8 @@
 // share (attn_core.hpp) would leave three of them without rows; here the waves share the keys instead:
 // wave w attends all rows to chunks w, w + 4, .. of 32 keys (two pages), and the four results are
 // joined at the end.  A wave's codes come by DMA, whole 1 KiB runs, into a ring that only it touches, so
-// the loop has no barrier, and are widened when they are read.  Arithmetic and operand layouts are
+// the loop has no barrier, and are widened when they are read.  (24 sequences of up to 4000 tokens, 1 to 8 new
+// each, 32 heads over 8: 101 MB in 27 us, 3.7 TB/s; with the tiles of attn_core.hpp 53.)  Arithmetic and operand layouts are
 // those of attn_core.hpp: S^T = K Q^T, O^T += V^T P^T with v_mfma_f32_32x32x16.
 #pragma once
 

@@ -7,7 +7,9 @@
 // the records (attn_merge.hpp).  The grid holds every tile that there may be, and every part of a sequence; what has
 // nothing to do lies together at the end of its kind: workgroups go to the XCDs and to the shader engines
 // in turn, and a regular pattern of empty ones left half of those idle (4 prefixes of 18000 tokens, 16 members each: 70
-// us, 50 so).
+// us, 50 so).  16 groups of 16 sequences, 1808 shared tokens and up to 2500 of their own, 32 heads over 8: 719 MB in
+// 161 us, 4.5 TB/s, near the rate of a large copy; 4 of 32 with 18000 + up to 1500: 187 MB, 39 GFLOP in 80 us,
+// the prefixes' products on 256 workgroups, one a CU, that share no tile.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
