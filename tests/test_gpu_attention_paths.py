@@ -224,3 +224,32 @@ def test_a_row_whose_scores_are_all_minus_infinity(fp8rl, new, length):
     prompt[1, 2] = 0.0
     check(out, res, length, attention.FP8_VALUES, "chunk")
     assert torch.isfinite(prompt).all()
+
+
+@pytest.mark.parametrize("count", [255, 256, 257, 600])
+def test_many_short_sequences(fp8rl, count):
+    """The tiles' search looks at 256 sequences a step: counts on both sides of that, and more; none, one or more tiles each."""
+    announce(f"chunk and shared: {count} sequences or groups")
+    rng = np.random.default_rng(count)
+    new = rng.choice([0, 1, 2, 40], count, p=[0.3, 0.4, 0.28, 0.02])
+    new[-1] = 3
+    lens = new + rng.integers(0, 20, count)
+    kc, vc, table = paged(rng, lens, 1)
+    cu = offsets(new)
+    q = bf16(rng, (int(cu[-1]), 4, 128))
+    out = fp8rl.fp8rl_attention_prompt_fp8kv(q.cuda(), *chunk_args(kc, vc, table, lens, cu, int(lens.max())))
+    sizes = rng.integers(0, 3, count)
+    sizes[0], sizes[-1] = 1, 2
+    go = offsets(sizes)
+    lens2 = rng.integers(0, 50, int(go[-1]))
+    prefix = rng.integers(0, 50, count)
+    kc2, vc2, table2 = paged(rng, lens2, 1)
+    q2 = bf16(rng, (int(go[-1]), 4, 128))
+    shared = fp8rl.fp8rl_attention_decode_shared_fp8kv(
+        q2.cuda(), torch.from_numpy(kc2).cuda(), torch.from_numpy(vc2).cuda(), i32(table2), i32(lens2), i32(go), i32(prefix),
+        48, 50, f32_1(KS), f32_1(VS), SM)
+    torch.cuda.synchronize()
+    check(out, attention.prompt_paged(u16(q), kc, vc, KS, VS, table, lens, cu, SM), 60, attention.FP8_VALUES, "chunk")
+    seen = attention.shared_table(table2, lens2, go, prefix, 48)
+    check(shared, attention.prompt_paged(u16(q2), kc2, vc2, KS, VS, seen, lens2, np.arange(len(lens2) + 1), SM), 50,
+          attention.FP8_VALUES, "shared")
