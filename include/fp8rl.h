@@ -461,8 +461,8 @@ int fp8rl_attention_decode_bf16kv(const uint16_t* q, const uint16_t* k_cache, co
  *      read by no sequence and written by none.
  * What a row does not attend to does not reach it, NaN and infinities among later tokens' values
  * included; a row whose scores are all -inf gives NaN.
- * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; total * q_heads / 128 + 3 * batch * kv_heads < 2^23
- * (else FP8RL_ERR_UNSUPPORTED_SHAPE).  total == 0 or batch == 0 is a no-op.
+ * q_heads / kv_heads in {1, 2, 4, 8}; head_dim 128; batch <= 65535; total * q_heads / 128 + 4 * batch *
+ * kv_heads < 2^23 (else FP8RL_ERR_UNSUPPORTED_SHAPE).  total == 0 or batch == 0 is a no-op.
  * Alignment: q, k, v, out 16-byte, every ld a multiple of 8, cu_seqlens 4-byte.
  */
 int fp8rl_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t* k, int64_t ld_k, const uint16_t* v,

@@ -28,7 +28,7 @@ int check_prompt(const uint16_t* q, int64_t ld_q, const int32_t* cu_seqlens, int
   if (batch < 0 || total < 0) return FP8RL_ERR_INVALID_ARG;
   const int st = check_heads(q_heads, kv_heads, head_dim, sm_scale);
   if (st != kLaunch) return st;
-  if (batch >= kMaxDim || total >= kMaxDim) return FP8RL_ERR_UNSUPPORTED_SHAPE;
+  if (batch > 65535 || total >= kMaxDim) return FP8RL_ERR_UNSUPPORTED_SHAPE;
   if (batch == 0 || total == 0) return FP8RL_OK;
   if (fp8rl::attn_prompt_workgroups(batch, total, q_heads / kv_heads, kv_heads, fp8) >= kMaxGrid)
     return FP8RL_ERR_UNSUPPORTED_SHAPE;
@@ -99,7 +99,7 @@ int fp8rl_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t*
 
 int64_t fp8rl_attention_prompt_workspace_size(int64_t batch, int64_t total, int64_t q_heads, int64_t kv_heads,
                                               int64_t max_seq_len) {
-  if (batch < 1 || total < 1 || batch >= kMaxDim || total >= kMaxDim || max_seq_len < 0 ||
+  if (batch < 1 || total < 1 || batch > 65535 || total >= kMaxDim || max_seq_len < 0 ||
       max_seq_len >= (int64_t(1) << 30) || !group_ok(q_heads, kv_heads))
     return 0;
   const fp8rl::PromptSplit sp = fp8rl::attn_prompt_split(batch, total, q_heads / kv_heads, kv_heads, max_seq_len);

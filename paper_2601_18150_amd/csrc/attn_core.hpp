@@ -57,8 +57,28 @@ __device__ __forceinline__ int run_tiles(int rows, int small) {
   return rows <= small ? (rows + 31) >> 5 : (rows + 127) >> 7;
 }
 
+// Tiles of up to kScanned sequences are numbered one behind the other, and every wave counts them.  With more
+// that would be most of the work (65535 prompts of one token: 77 ms, 3.8 so; 1024 of 32 tokens 225 us, 149 so), and the sequences get places by their offsets
+// alone: sequence b's start at place(b) and are no more than place(b + 1) - place(b), of which some stay empty.
+// (A place more every third sequence: places that are empty at regular distances would leave the same shader engines idle.)
+constexpr int kScanned = 256;
+
+struct Places {
+  int shift, step;             // rows a place; further places a sequence
+
+  __host__ __device__ Places(int64_t rows, int64_t count, int small) {
+    // tiles of 128 rows, and up to three of 32 for a run that takes those; or places of 32 rows for all
+    const int few = (small + kRowsPerWave - 1) / kRowsPerWave;
+    const bool wide = small == 0 || rows / kAttnRows + few * count <= rows / kRowsPerWave + count;
+    shift = wide ? 7 : 5;
+    step = wide && small > 0 ? few : 1;
+  }
+  template <class T>
+  __host__ __device__ T operator()(T row, T b) const { return (row >> shift) + step * b + b / 3; }
+};
+
 // Sequence of tile `t`, each with ceil(length * G / rows of a tile) of them, and the tile's index inside it.
-// Offsets are clamped into [0, total], lengths below 0 count as 0.  false: behind the last tile.
+// Offsets are clamped into [0, total], lengths below 0 count as 0.  false: no such tile.
 struct TileOf {
   int b, index, first, n;      // sequence, tile inside it, its first token, its tokens
 
@@ -70,50 +90,68 @@ struct TileOf {
   }
 };
 
-// (total rows < 2^30.  256 sequences at a time, four a lane: with one a lane 1024 prompts of 32 tokens took 225 us, 183 so.)
+// (total rows < 2^30; four sequences a lane.)
 __device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int total, int group_log2, int small, int t, TileOf& out) {
   constexpr int kPerLane = 4;
+  static_assert(kScanned == 64 * kPerLane, "one step");
   const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int base = 0; base < count; base += 64 * kPerLane) {
-    const int first = base + kPerLane * lane;
-    int at[kPerLane + 1], n[kPerLane], tiles[kPerLane], mine = 0;
-#pragma unroll
-    for (int u = 0; u <= kPerLane; ++u) at[u] = offsets[min(first + u, count)];
-#pragma unroll
-    for (int u = 0; u <= kPerLane; ++u) at[u] = min(max(at[u], 0), total);
-#pragma unroll
-    for (int u = 0; u < kPerLane; ++u) {                   // (behind the last sequence: at[count] - at[count])
-      n[u] = max(at[u + 1] - at[u], 0);
-      tiles[u] = run_tiles(n[u] << group_log2, small);
-      mine += tiles[u];
+  auto offset = [&](int i) { return min(max(offsets[i], 0), total); };
+  if (count > kScanned) {                                  // the last sequence whose place is not above t, by 64 probes at a time
+    const Places place((int64_t)total << group_log2, count, small);
+    int lo = 0, n = count;
+    for (;;) {
+      const int stride = (n + 63) / 64;
+      const int i = lo + lane * stride;
+      const int at = min(i, count - 1);
+      const int below = __popcll(__ballot(i < lo + n && place(offset(at) << group_log2, at) <= t));
+      if (below == 0) return false;
+      lo += (below - 1) * stride;
+      n = min(stride, count - lo);
+      if (stride == 1) break;
     }
-    // (runs that overlap may have more tiles than the grid: kept from an overflow)
-    const int sum = wave_inclusive_sum(min(mine, 1 << 24));
-    const uint64_t hit = __ballot(before + sum > t);
-    if (hit) {
-      const int w = __builtin_ctzll(hit);
-      int r = t - before - (w > 0 ? __builtin_amdgcn_readlane(sum, w - 1) : 0);
+    out.b = lo;
+    out.first = offset(lo);
+    out.n = max(offset(lo + 1) - out.first, 0);
+    out.index = t - place(out.first << group_log2, lo);
+    return out.index >= 0 && out.index < run_tiles(out.n << group_log2, small);
+  }
+  const int first = kPerLane * lane;
+  int at[kPerLane + 1], n[kPerLane], tiles[kPerLane], mine = 0;
 #pragma unroll
-      for (int u = 0; u < kPerLane; ++u) {
-        const int here = __builtin_amdgcn_readlane(tiles[u], w);
-        if (r < here) {
-          out.b = base + kPerLane * w + u;
-          out.index = r;
-          out.first = __builtin_amdgcn_readlane(at[u], w);
-          out.n = __builtin_amdgcn_readlane(n[u], w);
-          return true;
-        }
-        r -= here;
-      }
+  for (int u = 0; u <= kPerLane; ++u) at[u] = offsets[min(first + u, count)];
+#pragma unroll
+  for (int u = 0; u <= kPerLane; ++u) at[u] = min(max(at[u], 0), total);
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {                     // (behind the last sequence: at[count] - at[count])
+    n[u] = max(at[u + 1] - at[u], 0);
+    tiles[u] = run_tiles(n[u] << group_log2, small);
+    mine += tiles[u];
+  }
+  // (runs that overlap may have more tiles than the grid: kept from an overflow)
+  const int sum = wave_inclusive_sum(min(mine, 1 << 24));
+  const uint64_t hit = __ballot(sum > t);
+  if (hit == 0) return false;
+  const int w = __builtin_ctzll(hit);
+  int r = t - (w > 0 ? __builtin_amdgcn_readlane(sum, w - 1) : 0);
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    const int here = __builtin_amdgcn_readlane(tiles[u], w);
+    if (r < here) {
+      out.b = kPerLane * w + u;
+      out.index = r;
+      out.first = __builtin_amdgcn_readlane(at[u], w);
+      out.n = __builtin_amdgcn_readlane(n[u], w);
+      return true;
     }
-    before += __builtin_amdgcn_readlane(sum, 63);
+    r -= here;
   }
   return false;
 }
 
-// Tiles of all runs: an upper bound (each run's last one may be partly filled).
-inline int64_t attn_tile_bound(int64_t rows, int64_t runs, int small) {
+// Tiles that the grid has to hold for `rows` rows of `count` sequences, of which `tokens` at most are not empty.
+inline int64_t attn_tile_bound(int64_t rows, int64_t count, int64_t tokens, int small) {
+  if (count > kScanned) return Places(rows, count, small)(rows, count);
+  const int64_t runs = count < tokens ? count : tokens;    // (the last tile of each may be partly filled)
   if (small == 0) return rows / kAttnRows + runs;
   const int64_t mixed = rows / kAttnRows + runs * ((small + kRowsPerWave - 1) / kRowsPerWave);
   const int64_t all_small = rows / kRowsPerWave + runs;

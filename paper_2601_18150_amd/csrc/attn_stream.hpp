@@ -61,7 +61,7 @@ __device__ __forceinline__ void stream_read(const uint8_t* ks, const int (&key_o
       : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(a[4]), "=&v"(a[5]), "=&v"(a[6]), "=&v"(a[7]), "=&v"(w[0]),
         "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7])
       : "v"(k + key_off[0]), "v"(k + key_off[1]), "v"(k + key_off[2]), "v"(k + key_off[3]), "v"(k + key_off[4]),
-        "v"(k + key_off[5]), "v"(k + key_off[6]), "v"(k + key_off[7]), "v"(v), "v"(v + 1024), "v"(v + 2048), "v"(v + 3072)
+        "v"(k + key_off[5]), "v"(k + key_off[6]), "v"(k + key_off[7]), "v"(v), "v"(v + 1024), "v"(v + 2 * 1024), "v"(v + 3 * 1024)
       : "memory");
 #pragma unroll
   for (int i = 0; i < 8; ++i) {

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kFew ? 256 : 32 * kMergeSets) void attn_prompt_merg
 }  // namespace
 
 int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, bool fp8) {
-  return attn_tile_bound(total * group, batch < total ? batch : total, fp8 ? kPromptSmall : 0) * kv_heads;
+  return attn_tile_bound(total * group, batch, total, fp8 ? kPromptSmall : 0) * kv_heads;
 }
 
 // Splits of the keys where the tiles alone are too few for the 512 workgroups that the chip holds: as many as

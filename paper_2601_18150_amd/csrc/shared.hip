@@ -245,7 +245,7 @@ SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int6
 }
 
 static int64_t prefix_tiles(int64_t batch, int64_t groups, int64_t group) {
-  return attn_tile_bound(batch * group, groups < batch ? groups : batch, kSharedSmall);
+  return attn_tile_bound(batch * group, groups, batch, kSharedSmall);
 }
 
 int64_t attn_shared_workgroups(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,

@@ -92,7 +92,7 @@ int main() {
         {A, 1024, A, 256, A, 256, A, 3, 100, 8, 2, 128, 0, A, 1024},
         {{0, 0, ARG}, {0, A + 2, ALIGN}, {1, 1016, ARG}, {1, 1025, ALIGN}, {2, 0, ARG}, {2, A + 8, ALIGN}, {3, 248, ARG},
          {3, 257, ALIGN}, {3, 1 << 24, SHAPE}, {4, 0, ARG}, {4, A + 8, ALIGN}, {5, 0, ARG}, {5, 260, ALIGN},
-         {5, HUGE62, SHAPE}, {6, 0, ARG}, {6, A + 2, ALIGN}, {7, -1, ARG}, {7, 0, OK}, {7, BIG, SHAPE}, {7, 1 << 23, SHAPE},
+         {5, HUGE62, SHAPE}, {6, 0, ARG}, {6, A + 2, ALIGN}, {7, -1, ARG}, {7, 0, OK}, {7, BIG, SHAPE}, {7, 1 << 23, SHAPE}, {7, 65536, SHAPE},
          {8, -1, ARG}, {8, 0, OK}, {8, BIG - 1, SHAPE}, {8, HUGE62, SHAPE}, {9, 0, ARG}, {9, 3, SHAPE}, {9, 6, SHAPE},
          {9, 32, SHAPE}, {10, 0, ARG}, {10, -2, ARG}, {10, 3, SHAPE}, {11, 64, SHAPE}, {11, 0, SHAPE}, {12, 1, ARG},
          {12, 2, ARG}, {12, 3, ARG}, {12, 4, ARG}, {13, 0, ARG}, {13, A + 4, ALIGN}, {14, 1000, ARG}, {14, 1028, ALIGN},

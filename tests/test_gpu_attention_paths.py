@@ -253,3 +253,37 @@ def test_many_short_sequences(fp8rl, count):
     seen = attention.shared_table(table2, lens2, go, prefix, 48)
     check(shared, attention.prompt_paged(u16(q2), kc2, vc2, KS, VS, seen, lens2, np.arange(len(lens2) + 1), SM), 50,
           attention.FP8_VALUES, "shared")
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (4, 2)])
+def test_many_prompts(fp8rl, heads, kv_heads):
+    """More prompts than are counted one by one: empty ones, whole tiles, a few long ones, rows in front and behind."""
+    announce(f"prompt: 400 sequences, {heads}/{kv_heads} heads")
+    rng = np.random.default_rng(heads)
+    lengths = rng.choice([0, 1, 16, 32, 33, 300], 400, p=[0.3, 0.3, 0.19, 0.1, 0.1, 0.01])
+    cu = offsets(lengths, 3)
+    n = int(cu[-1]) + 5
+    q, k, v = bf16(rng, (n, heads, 128)), bf16(rng, (n, kv_heads, 128)), bf16(rng, (n, kv_heads, 128))
+    out = torch.full((n, heads, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    fp8rl.fp8rl_attention_prompt_bf16(q.cuda(), k.cuda(), v.cuda(), i32(cu), 0.09, out=out)
+    torch.cuda.synchronize()
+    check(out, attention.prompt(u16(q), u16(k), u16(v), cu, 0.09), 300, attention.BF16_VALUES, "prompt")
+    assert torch.all(out[:3] == 9.0) and torch.all(out[int(cu[-1]):] == 9.0)
+
+
+@pytest.mark.parametrize("go,prefix,max_prefix", [([0, 3], [64], 0), ([1, 1, 1], [64, 64], 64), ([0, 3], [-5], 64), ([3, 3], [64], 64)])
+def test_nothing_shared(fp8rl, go, prefix, max_prefix):
+    announce(f"shared: groups {go}, prefixes {prefix}, at most {max_prefix}; a negative length")
+    rng = np.random.default_rng(5)
+    lens = [90, 33, 70]
+    kc, vc, table = paged(rng, lens, 2)
+    q = bf16(rng, (3, 4, 128))
+    out = fp8rl.fp8rl_attention_decode_shared_fp8kv(
+        q.cuda(), torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda(), i32(table), i32([90, -7, 70]), i32(go), i32(prefix),
+        max_prefix, 90, f32_1(KS), f32_1(VS), SM)
+    chunk = fp8rl.fp8rl_attention_prompt_fp8kv(q.cuda(), *chunk_args(kc, vc, table, [90, -7, 70], [0, 1, 2, 3], 90))
+    torch.cuda.synchronize()
+    res = attention.prompt_paged(u16(q), kc, vc, KS, VS, table, [90, 0, 70], [0, 1, 2, 3], SM)
+    check(out, res, 90, attention.FP8_VALUES, "shared")
+    check(chunk, res, 90, attention.FP8_VALUES, "chunk")
+    assert torch.all(out[1] == 0) and torch.all(chunk[1] == 0)
