@@ -645,13 +645,12 @@ def fp8rl_attention_decode_bf16kv(q, k_cache, v_cache, block_table, seq_lens, ma
 
 def _head_rows(x: torch.Tensor, what: str):
     """Row pitch of a bf16 [tokens][heads][128] tensor whose heads lie side by side."""
-    if x.dtype != torch.bfloat16 or x.dim() != 3:
+    if x.dtype is not torch.bfloat16 or x.dim() != 3:
         raise TypeError(f"{what} must be bfloat16 [tokens][heads][head_dim]")
     t, h, d = x.shape
     pitch, head, col = x.stride()
-    if (d > 1 and col != 1) or (h > 1 and head != d):
-        if t > 0 and h > 0:
-            raise ValueError(f"the heads of a token of {what} must lie side by side")
+    if (col != 1 and d > 1 or head != d and h > 1) and t > 0 and h > 0:
+        raise ValueError(f"the heads of a token of {what} must lie side by side")
     return pitch if t > 1 else h * d
 
 
@@ -666,7 +665,7 @@ def _here(*ts):
 
 
 def _i32(x: torch.Tensor, n, what: str):
-    if x.dtype != torch.int32 or x.dim() != 1 or not x.is_contiguous() or (n is not None and x.shape[0] != n):
+    if x.dtype is not torch.int32 or x.dim() != 1 or not x.is_contiguous() or (n is not None and x.shape[0] != n):
         raise ValueError(f"{what} must be contiguous int32 [{'n' if n is None else n}]")
 
 
@@ -701,7 +700,8 @@ def _empty(shape, dtype, device, stream):
 
 def _out_rows(out, q, stream):
     if out is None:
-        return _empty(q.shape, torch.bfloat16, q.device, stream)
+        # (empty_like: half the time of empty with a shape; dense, also where q has a pitch)
+        return torch.empty_like(q) if stream is None else _empty(q.shape, torch.bfloat16, q.device, stream)
     if out.shape != q.shape:
         raise ValueError("out must have q's shape")
     return out
@@ -814,6 +814,9 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
     return out
 
 
+_nbytes = operator.attrgetter("nbytes")
+
+
 def _cache_list(caches):
     """(array of base pointers, their number, bytes per block, blocks) of contiguous caches of one size, the first of
     them [num_blocks][..]."""
@@ -822,7 +825,7 @@ def _cache_list(caches):
     first = caches[0]
     blocks, size = (first.shape[0] if first.dim() > 1 else -1), first.nbytes
     # (a model has a hundred caches: no Python step for each, and what takes longest, their shapes, is left out)
-    if blocks < 0 or set(map(operator.attrgetter("nbytes"), caches)) != {size} or \
+    if blocks < 0 or set(map(_nbytes, caches)) != {size} or \
             not all(map(torch.Tensor.is_contiguous, caches)):
         raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
     return array.array("Q", map(torch.Tensor.data_ptr, caches)), len(caches), size // max(blocks, 1), blocks
