@@ -572,8 +572,9 @@ __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8]
 // The same from the FP8 cache, through registers, where the codes are widened: a tile's codes are asked
 // for when those of the one before it have been stored, its page ids a step earlier.  What is asked for
 // behind the last tile repeats the last pages.  (The codes held in registers leave room for two
-// workgroups on a CU; brought through LDS by DMA instead, three of them took as long over long
-// contexts and a tenth longer over short ones.  Codes asked for two tiles ahead: the same time.)  Three
+// workgroups on a CU; three took longer, with the codes brought through LDS by DMA by 5 to 10%, with the
+// codes asked for and stored around the value product alone by 4 to 13%: a tile moves 160 KB through LDS, 1280 cycles
+// of it.  Codes asked for two tiles ahead: the same time.)  Three
 // chunks of 2048 against up to 18432 tokens: 1.15 ms, 0.98 PFLOP/s; the widening adds a fifth to the vector work,
 // which a CU with two workgroups overlaps less.
 __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
