@@ -165,6 +165,32 @@ inline int64_t attn_tile_guess(int64_t rows, int64_t runs, int small) {
   return runs * ((mean + tile - 1) / tile);
 }
 
+// Keys of each of n shares of `keys`: whole tiles, 256 at least.
+inline int64_t attn_share(int64_t keys, int64_t n) {
+  const int64_t share = ((keys + n - 1) / n + kTileKeys - 1) / kTileKeys * kTileKeys;
+  return share < 256 ? 256 : share;
+}
+
+// In how many shares of the keys `wgs` workgroups end first, by what was measured (us): 64 keys of a workgroup alone on a
+// CU and beside another, 5 for its start and end, the launch that joins shares where there would be none, a share's records.
+// weight: of the sum of a CU's workgroups (below 1 where they differ); the longest is a bound, and reading the cache.
+struct ShareCost { double alone, beside, join, record, weight, read; };
+
+inline int64_t attn_shares(int64_t wgs, int64_t keys, const ShareCost& c) {
+  const int64_t most = (keys + 255) / 256;
+  int64_t best = 1;
+  double least = 0.0;
+  for (int64_t n = 1; n == 1 || (n <= most && (n - 1) * wgs < 768); ++n) {
+    const int64_t tiles = attn_share(keys, n) / kTileKeys, on_cu = (wgs * n + 255) / 256;
+    const double one = (on_cu > 1 ? c.beside : c.alone) * tiles + 5.0;
+    const double all = on_cu / 2 * (c.beside * tiles + 5.0) + on_cu % 2 * (c.alone * tiles + 5.0);
+    const double busy = one > c.weight * all ? one : c.weight * all;
+    const double us = (busy > c.read ? busy : c.read) + n * c.record + (n > 1 ? c.join : 0.0);
+    if (n == 1 || us < least) best = n, least = us;
+  }
+  return best;
+}
+
 inline int group_log2_of(int64_t g) { return g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3; }
 
 // Rows of the workgroup as this lane sees its own (lane % 32 of its wave).

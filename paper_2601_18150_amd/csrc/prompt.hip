@@ -177,36 +177,18 @@ int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int6
   return attn_tile_bound(total * group, batch, total, fp8 ? kPromptSmall : 0) * kv_heads;
 }
 
-// Splits of the keys, 256 at least each, as if the sequences were all as long as their mean and had max_seq_len keys.
-// Small tiles, bound by reading: as many as fill the 512 places that the chip holds.  Large ones: as many as end
-// first by what was measured of one (us): 64 keys 1.5 alone on a CU, 2.6 beside another, its start and end 5; the joining
-// launch 4, and the records at 5 TB/s.  Sequences differ, so a CU's share counts 0.8 of that, and the longest workgroup
-// as a bound.  (Against 512 places for all, us: 4 chunks of up to 375 behind 707 tokens, 32 heads over 4, 45 -> 38; one of 429
-// behind 334, 64 over 8, 39 -> 29; two of 239 behind 3926 66 -> 68; 13 of up to 777 behind 3001 84 -> 83.  A share
-// counted whole: 83 -> 88 there, 0.5 of it: 38 -> 45 for one of 601 behind 157.)
+// Splits of the keys, as if the sequences were all as long as their mean and had max_seq_len keys.  Small tiles, bound
+// by reading: as many as fill the 512 places that the chip holds.  Large ones: as many as end first (attn_shares), records
+// at 5 TB/s.  (Against 512 places for all, us: 4 chunks of up to 375 behind 707 tokens, 32 heads over 4, 45 -> 38; one of 429
+// behind 334, 64 over 8, 39 -> 29; two of 239 behind 3926 66 -> 68; 13 of up to 777 behind 3001 84 -> 83.  A CU's
+// workgroups weighed in full instead of 0.8: 83 -> 88 there, 0.5: 38 -> 45 for one of 601 behind 157.)
 PromptSplit attn_prompt_split(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t max_seq_len) {
   const int64_t runs = batch < total ? batch : total;
   const int64_t wgs = attn_tile_guess(total * group, runs, kPromptSmall) * kv_heads;
-  const int64_t most = (max_seq_len + 255) / 256;        // (splits)
-  auto keys_of = [&](int64_t n) {
-    const int64_t keys = ((max_seq_len + n - 1) / n + kTileKeys - 1) / kTileKeys * kTileKeys;
-    return keys < 256 ? 256 : keys;
-  };
-  int64_t splits = 1;
-  if (total * group <= runs * kPromptSmall) {
-    splits = wgs > 0 ? (512 + wgs - 1) / wgs : 1;
-  } else {
-    const double record = total * group * kv_heads * (4.0 * (kHeadDim + 2)) / 5e6;
-    double best = 0.0;
-    for (int64_t n = 1; n == 1 || (n <= most && (n - 1) * wgs < 768); ++n) {
-      const int64_t tiles = keys_of(n) / kTileKeys, on_cu = (wgs * n + 255) / 256;
-      const double one = (on_cu > 1 ? 2.6 : 1.5) * tiles + 5.0;
-      const double all = on_cu / 2 * (2.6 * tiles + 5.0) + on_cu % 2 * (1.5 * tiles + 5.0);
-      const double us = (one > 0.8 * all ? one : 0.8 * all) + (n > 1 ? 4.0 + n * record : 0.0);
-      if (n == 1 || us < best) splits = n, best = us;
-    }
-  }
-  const int64_t keys = keys_of(splits);
+  int64_t splits = wgs > 0 ? (512 + wgs - 1) / wgs : 1;
+  if (total * group > runs * kPromptSmall)
+    splits = attn_shares(wgs, max_seq_len, {1.5, 2.6, 4.0, total * group * kv_heads * (4.0 * (kHeadDim + 2)) / 5e6, 0.8, 0.0});
+  const int64_t keys = attn_share(max_seq_len, splits);
   splits = (max_seq_len + keys - 1) / keys;
   PromptSplit s;
   s.splits = splits > 1 ? (int)splits : 1;

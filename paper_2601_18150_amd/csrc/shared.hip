@@ -216,22 +216,24 @@ __global__ __launch_bounds__(kFew ? 256 : 32 * kMergeSets) void attn_shared_merg
 
 }  // namespace
 
-// Records of a sequence and kv head.  The prefixes' keys are split where their tiles alone are few, 256 keys
-// each at least, so that there are about 256 workgroups of them: the chip holds 512, and what is left over goes to
-// the sequences' own tokens, which are bound by reading, meanwhile (us for 192 / 256 / 384 / 512: 4 x 32 sequences of
-// 18000 + up to 1500 tokens, large tiles, 93 / 80 / 85 / 91; 2 x 64 of 8000 + 1500 73 / 73 / 80 / 86; small tiles, 16 x
-// 16 of 1800 + 2500, - / 160 / 170 / 170).  Own tokens are split where the sequences are fewer than 1024, 256
-// tokens each at least (8 x 16 of 4000 + up to 800 tokens, for 512 / 1024 / 2048: 51 / 50 / 55; 4 x 32 as above 80 /
-// 80 / 87).
+// Records of a sequence and kv head.  The prefixes' keys go into as many shares as end first (attn_shares), where two
+// workgroups on a CU take twice as long as one, no longer than it takes to read the cache at 4.7 TB/s, and records,
+// which the joining launch reads again, count three times; what the prefixes leave free goes to the sequences' own tokens
+// meanwhile.  (Against 256 workgroups, rounded up, us: 6 x 11 sequences of 11040 + 8 tokens, 64 heads over 8, 79 -> 60; 3 x
+// 21 of 11936 + 74, 32 over 4, 56 -> 49; 9 x 16 of 9424 + 4, 16 over 8, 50 -> 44; 6 x 23 of 11936 + 1416, 32 over 8,
+// 128 -> 132; 4 x 32 of 18000 + 1500 and 16 x 16 of 1808 + 2500 as before, 78 and 160.  512 workgroups: 91 and 170.)
+// Own tokens are split where the sequences are fewer than 1024, 256 tokens each at least (8 x 16 of 4000 + up to 800
+// tokens, for 512 / 1024 / 2048: 51 / 50 / 55; 4 x 32 as above 80 / 80 / 87).
 SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,
                               int64_t max_seq_len) {
   const int64_t runs = groups < batch ? groups : batch;
   const int64_t wgs = attn_tile_guess(batch * group, runs, kSharedSmall) * kv_heads;
-  int64_t splits = wgs > 0 ? (256 + wgs - 1) / wgs : 1;
-  int64_t keys = (max_prefix_len + splits - 1) / splits;
-  keys = (keys + kTileKeys - 1) / kTileKeys * kTileKeys;
-  if (keys < 256) keys = 256;
-  splits = (max_prefix_len + keys - 1) / keys;
+  const bool small = batch * group <= runs * kSharedSmall;
+  const double record = 3 * batch * group * kv_heads * (4.0 * (kHeadDim + 2)) / 5e6;
+  const double read = runs * max_prefix_len * kv_heads * (2.0 * kHeadDim) / 4.7e6;
+  const ShareCost cost{small ? 0.47 : 1.5, small ? 0.94 : 3.0, 0.0, record, 1.0, read};
+  const int64_t keys = attn_share(max_prefix_len, attn_shares(wgs, max_prefix_len, cost));
+  const int64_t splits = (max_prefix_len + keys - 1) / keys;
   const int64_t pairs = batch * kv_heads;
   int64_t own = (1024 + pairs - 1) / pairs;
   const int64_t most = (max_seq_len + kOwnMinPages * kPageTokens - 1) / (kOwnMinPages * kPageTokens);
