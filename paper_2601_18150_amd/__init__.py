@@ -672,19 +672,20 @@ def _i32(x: torch.Tensor, n, what: str):
 def _paged(k_cache, v_cache, block_table):
     """Checked FP8 caches and block table: (k, v, num_blocks, kv_heads)."""
     k_cache, v_cache = _u8(k_cache), _u8(v_cache)
-    if k_cache.dim() < 2 or not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+    k, v = k_cache.shape, v_cache.shape
+    if len(k) < 2 or len(v) < 2 or not (k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise ValueError("the caches must be contiguous [num_blocks][kv_heads][..]")
-    blocks, kv_heads = k_cache.shape[:2]
-    if v_cache.shape[:2] != (blocks, kv_heads) or not k_cache.numel() == v_cache.numel() == blocks * kv_heads * 2048:
+    blocks, kv_heads = k[0], k[1]
+    if v[0] != blocks or v[1] != kv_heads or not k_cache.numel() == v_cache.numel() == blocks * kv_heads * 2048:
         raise ValueError("the caches must hold 16 x 128 codes per block and kv head")
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
         raise ValueError("block_table must be contiguous int32 [batch][max_blocks]")
     return k_cache, v_cache, blocks, kv_heads
 
 
 def _scale1(*scales):
     for s in scales:
-        if s.dtype != torch.float32 or s.numel() != 1:
+        if s.dtype is not torch.float32 or s.numel() != 1:
             raise ValueError("k_scale and v_scale must be fp32 [1]")
 
 
@@ -766,7 +767,7 @@ def fp8rl_attention_prompt_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, v_cache
                                              block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(),
                                              cu_seqlens.data_ptr(), batch, total, q_heads, kv_heads, dim, int(max_seq_len),
                                              k_scale.data_ptr(), v_scale.data_ptr(), float(sm_scale), out.data_ptr(),
-                                             ld_out, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                             ld_out, workspace.data_ptr(), workspace.nbytes,
                                              _stream(stream))
     _check(name, st)
     return out
@@ -809,7 +810,7 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_blocks, block_table.data_ptr(), block_table.shape[1],
         seq_lens.data_ptr(), batch, group_offsets.data_ptr(), prefix_lens.data_ptr(), groups, int(max_prefix_len), q_heads,
         kv_heads, dim, int(max_seq_len), k_scale.data_ptr(), v_scale.data_ptr(), float(sm_scale), out.data_ptr(),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+        workspace.data_ptr(), workspace.nbytes, _stream(stream))
     _check(name, st)
     return out
 
@@ -894,7 +895,7 @@ def fp8rl_kv_compact(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, 
     _here(*caches, block_table, seq_lens, block_refs, live, workspace)
     _check("fp8rl_kv_compact", load().fp8rl_kv_compact(
         ptrs.buffer_info()[0], n, size, blocks, block_table.data_ptr(), *block_table.shape, seq_lens.data_ptr(),
-        block_refs.data_ptr(), live.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        block_refs.data_ptr(), live.data_ptr(), workspace.data_ptr(), workspace.nbytes,
         _stream(stream)))
     return live
 
