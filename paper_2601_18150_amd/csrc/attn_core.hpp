@@ -180,13 +180,25 @@ inline int64_t attn_shares(int64_t wgs, int64_t keys, const ShareCost& c) {
   const int64_t most = (keys + 255) / 256;
   int64_t best = 1;
   double least = 0.0;
-  for (int64_t n = 1; n == 1 || (n <= most && (n - 1) * wgs < 768); ++n) {
+  auto consider = [&](int64_t n) {
     const int64_t tiles = attn_share(keys, n) / kTileKeys, on_cu = (wgs * n + 255) / 256;
     const double one = (on_cu > 1 ? c.beside : c.alone) * tiles + 5.0;
     const double all = on_cu / 2 * (c.beside * tiles + 5.0) + on_cu % 2 * (c.alone * tiles + 5.0);
     const double busy = one > c.weight * all ? one : c.weight * all;
     const double us = (busy > c.read ? busy : c.read) + n * c.record + (n > 1 ? c.join : 0.0);
     if (n == 1 || us < least) best = n, least = us;
+  };
+  consider(1);
+  if (most < 2 || wgs < 1 || wgs >= 768) return best;
+  // the largest number for each count of workgroups on a CU, and parts of the first
+  for (int64_t k = 1; (256 * k / wgs - 1) * wgs < 768; ++k) {
+    const int64_t n = 256 * k / wgs;
+    if (n > 1) consider(n < most ? n : most);
+    if (n >= most) break;
+  }
+  for (int64_t part = 3; 256 / wgs >= 4 && part > 0; --part) {
+    const int64_t n = 256 / wgs * part / 4;
+    if (n > 1 && n < most) consider(n);
   }
   return best;
 }
