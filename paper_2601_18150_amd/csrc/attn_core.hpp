@@ -51,10 +51,11 @@ __device__ __forceinline__ int value_at(int r, int c) { return r * 256 + ((c ^ (
 // (16-key step, half, dim), the eight keys of that half in the order of the value product.
 __device__ __forceinline__ int value16_at(int step, int h, int dim) { return ((step * 2 + h) * kHeadDim + dim) * 16; }
 
-// Tiles of a run of `rows`: of 128 rows, or of 32 where `small` says that so few rows take those.
-__device__ __forceinline__ int run_tiles(int rows, int small) {
-  static_assert(kRowsPerWave == 32 && kAttnRows == 128, "shifts");
-  return rows <= small ? (rows + 31) >> 5 : (rows + 127) >> 7;
+// Tiles of a run of `rows`: of 2^shift rows, or of 32 where `small` says that so few rows take those.
+constexpr int kAttnShift = 7, kHalfShift = 6;
+static_assert(kRowsPerWave == 32 && kAttnRows == 1 << kAttnShift, "shifts");
+__device__ __forceinline__ int run_tiles(int rows, int small, int shift) {
+  return rows <= small ? (rows + 31) >> 5 : (rows + (1 << shift) - 1) >> shift;
 }
 
 // Tiles of up to kScanned sequences are numbered one behind the other, and every wave counts them.  With more
@@ -66,11 +67,11 @@ constexpr int kScanned = 256;
 struct Places {
   int shift, step;             // rows a place; further places a sequence
 
-  __host__ __device__ Places(int64_t rows, int64_t count, int small) {
-    // tiles of 128 rows, and up to three of 32 for a run that takes those; or places of 32 rows for all
+  __host__ __device__ Places(int64_t rows, int64_t count, int small, int tile_shift) {
+    // large tiles, and up to three of 32 for a run that takes those; or places of 32 rows for all
     const int few = (small + kRowsPerWave - 1) / kRowsPerWave;
-    const bool wide = small == 0 || rows / kAttnRows + few * count <= rows / kRowsPerWave + count;
-    shift = wide ? 7 : 5;
+    const bool wide = small == 0 || (rows >> tile_shift) + few * count <= rows / kRowsPerWave + count;
+    shift = wide ? tile_shift : 5;
     step = wide && small > 0 ? few : 1;
   }
   template <class T>
@@ -91,13 +92,14 @@ struct TileOf {
 };
 
 // (total rows < 2^30; four sequences a lane.)
-__device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int total, int group_log2, int small, int t, TileOf& out) {
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int total, int group_log2, int small, int shift, int t,
+                                          TileOf& out) {
   constexpr int kPerLane = 4;
   static_assert(kScanned == 64 * kPerLane, "one step");
   const int lane = threadIdx.x & 63;
   auto offset = [&](int i) { return min(max(offsets[i], 0), total); };
   if (count > kScanned) {                                  // the last sequence whose place is not above t, by 64 probes at a time
-    const Places place((int64_t)total << group_log2, count, small);
+    const Places place((int64_t)total << group_log2, count, small, shift);
     int lo = 0, n = count;
     for (;;) {
       const int stride = (n + 63) / 64;
@@ -113,7 +115,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int
     out.first = offset(lo);
     out.n = max(offset(lo + 1) - out.first, 0);
     out.index = t - place(out.first << group_log2, lo);
-    return out.index >= 0 && out.index < run_tiles(out.n << group_log2, small);
+    return out.index >= 0 && out.index < run_tiles(out.n << group_log2, small, shift);
   }
   const int first = kPerLane * lane;
   int at[kPerLane + 1], n[kPerLane], tiles[kPerLane], mine = 0;
@@ -124,7 +126,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {                     // (behind the last sequence: at[count] - at[count])
     n[u] = max(at[u + 1] - at[u], 0);
-    tiles[u] = run_tiles(n[u] << group_log2, small);
+    tiles[u] = run_tiles(n[u] << group_log2, small, shift);
     mine += tiles[u];
   }
   // (runs that overlap may have more tiles than the grid: kept from an overflow)
@@ -149,11 +151,11 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int count, int
 }
 
 // Tiles that the grid has to hold for `rows` rows of `count` sequences, of which `tokens` at most are not empty.
-inline int64_t attn_tile_bound(int64_t rows, int64_t count, int64_t tokens, int small) {
-  if (count > kScanned) return Places(rows, count, small)(rows, count);
+inline int64_t attn_tile_bound(int64_t rows, int64_t count, int64_t tokens, int small, int shift) {
+  if (count > kScanned) return Places(rows, count, small, shift)(rows, count);
   const int64_t runs = count < tokens ? count : tokens;    // (the last tile of each may be partly filled)
-  if (small == 0) return rows / kAttnRows + runs;
-  const int64_t mixed = rows / kAttnRows + runs * ((small + kRowsPerWave - 1) / kRowsPerWave);
+  if (small == 0) return (rows >> shift) + runs;
+  const int64_t mixed = (rows >> shift) + runs * ((small + kRowsPerWave - 1) / kRowsPerWave);
   const int64_t all_small = rows / kRowsPerWave + runs;
   return mixed < all_small ? mixed : all_small;
 }
@@ -353,18 +355,22 @@ __device__ __forceinline__ void scale_if(uint64_t any, f32x16 (&o)[4], float alp
 // limit, which only the last tiles have.
 // P is rounded to the type of the values: against f16 values (E4M3 codes, exact there) 2^-12
 // relative, against bf16 ones 2^-9, of the size of the output's own rounding.
-template <bool kF16Values, bool kMask>
+template <bool kF16Values, bool kMask, int kBlocks = 2>
 __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int k0, float c,
-                                            const LaneOffsets<kF16Values>& lane_at, const uint8_t* keys, uint32_t (&p)[16]) {
+                                            const LaneOffsets<kF16Values>& lane_at, const uint8_t* keys,
+                                            uint32_t (&p)[8 * kBlocks]) {
   const LaneOffsets<kF16Values> at = lane_at.fresh();
   const int h = (threadIdx.x & 63) >> 5;
-  f32x16 s[2] = {(f32x16)(0.0f), (f32x16)(0.0f)};
+  f32x16 s[kBlocks];
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(keys, 8 * (i & 1) + (i >> 1)), q[i >> 1], s[i & 1], 0, 0, 0);
+  for (int b = 0; b < kBlocks; ++b) s[b] = (f32x16)(0.0f);
+#pragma unroll
+  for (int i = 0; i < 8 * kBlocks; ++i)
+    s[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(keys, 8 * (i % kBlocks) + i / kBlocks), q[i / kBlocks],
+                                                             s[i % kBlocks], 0, 0, 0);
   sched<kSchedLdsRead, 4>();
 #pragma unroll
-  for (int i = 0; i < 12; ++i) {
+  for (int i = 0; i < 8 * kBlocks - 4; ++i) {
     sched<kSchedMfma, 1>();
     sched<kSchedLdsRead, 1>();
   }
@@ -372,14 +378,14 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
   if constexpr (kMask) {
     const int from = row.limit - k0 - 4 * h;               // (key - k0 - 4 h above it: not visible)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (32 * b + 8 * (i >> 2) + (i & 3) > from) s[b][i] = -INFINITY;
   }
-  float mx = fmaxf(s[0][0], s[1][0]);
+  float mx = fmaxf(s[0][0], s[kBlocks - 1][kBlocks == 1]);
 #pragma unroll
-  for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(s[0][i], s[1][i]), mx);
+  for (int i = 1; i < 16; ++i) mx = fmaxf(kBlocks == 1 ? s[0][i] : fmaxf(s[0][i], s[kBlocks - 1][i]), mx);
   mx = half_max(mx);
   const bool grown = (mx - acc.m) * c > kMaxGrowth;       // (of this row alone: rows do not affect each other)
   const float m = grown ? mx : acc.m;
@@ -389,7 +395,7 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
   acc.l *= alpha;
   scale_if(__ballot(grown), acc.o, alpha);
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
       const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -mc));
@@ -400,19 +406,19 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
 }
 
 // O^T += V^T P^T over the tile's values in LDS.
-template <bool kF16Values>
-__device__ __forceinline__ void attn_values(AttnAcc& acc, const uint32_t (&p)[16], const LaneOffsets<kF16Values>& lane_at,
+template <bool kF16Values, int kBlocks = 2>
+__device__ __forceinline__ void attn_values(AttnAcc& acc, const uint32_t (&p)[8 * kBlocks], const LaneOffsets<kF16Values>& lane_at,
                                             const uint8_t* values) {
   const LaneOffsets<kF16Values> at = lane_at.fresh();
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 8 * kBlocks; ++i) {
     const int t = i >> 2;
     acc.o[i & 3] = value_mfma<kF16Values>(at.value(values, i), make_uint4(p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]), acc.o[i & 3]);
   }
   constexpr int kReads = kF16Values ? 1 : 2;
   sched<kSchedLdsRead, 3 * kReads>();
 #pragma unroll
-  for (int i = 0; i < 13; ++i) {
+  for (int i = 0; i < 8 * kBlocks - 3; ++i) {
     sched<kSchedMfma, 1>();
     sched<kSchedLdsRead, kReads>();
   }
@@ -565,33 +571,36 @@ struct TileLds {
   uint8_t* v;
 };
 
-template <bool kF16Values, class Keys, class Values>
+// kBlocks 1: of each tile the wave takes 32 keys, from key `from` on; lds begins with those.
+template <bool kF16Values, int kBlocks, class Keys, class Values>
 __device__ __forceinline__ void attn_run(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
-                                         float c, const TileLds& lds, Keys next_keys, Values next_values) {
+                                         float c, const TileLds& lds, int from, Keys next_keys, Values next_values) {
   c = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
   const LaneOffsets<kF16Values> at;
-  uint32_t p[16];
+  uint32_t p[8 * kBlocks];
   int k0 = begin;
   for (; k0 + kTileKeys - 1 <= row.all_limit; k0 += kTileKeys) {
     next_values(k0);
-    attn_scores<kF16Values, false>(acc, q, row, k0, c, at, lds.k, p);
+    attn_scores<kF16Values, false, kBlocks>(acc, q, row, k0 + from, c, at, lds.k, p);
     next_keys(k0 + kTileKeys);
-    attn_values<kF16Values>(acc, p, at, lds.v);
+    attn_values<kF16Values, kBlocks>(acc, p, at, lds.v);
   }
   for (; k0 < end; k0 += kTileKeys) {
     next_values(k0);
-    attn_scores<kF16Values, true>(acc, q, row, k0, c, at, lds.k, p);
+    attn_scores<kF16Values, true, kBlocks>(acc, q, row, k0 + from, c, at, lds.k, p);
     next_keys(k0 + kTileKeys);
-    attn_values<kF16Values>(acc, p, at, lds.v);
+    attn_values<kF16Values, kBlocks>(acc, p, at, lds.v);
   }
 }
 
+template <int kBlocks>
 __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
                                               float c, const Bf16Rows<false>& k, const Bf16Rows<true>& v,
-                                              const TileLds& lds) {
+                                              const TileLds& lds, int from = 0) {
   k.load(begin, lds.k);
   v.load(begin, lds.v);                                    // (the first tile's come with its keys)
-  attn_run<false>(acc, q, row, begin, end, c, lds, [&](int k0) {
+  const TileLds mine{lds.k + from * 256, lds.v + from * 256};
+  attn_run<false, kBlocks>(acc, q, row, begin, end, c, mine, from, [&](int k0) {
     wait_vmcnt<0>();
     lds_barrier();
     if (k0 < end) k.load(k0, lds.k);
@@ -625,7 +634,7 @@ __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8],
   at = after;                                              // of the tile whose values are asked for next
   store_keys(fk, lds.k);
   fetch_keys(pages, at, fk);
-  attn_run<true>(acc, q, row, begin, end, c, lds, [&](int k0) {
+  attn_run<true, 2>(acc, q, row, begin, end, c, lds, 0, [&](int k0) {
     lds_barrier();
     store_keys(fk, lds.k);
     fetch_keys(pages, after, fk);
@@ -723,6 +732,48 @@ __device__ __forceinline__ void attn_redo(AttnAcc& acc, const bf16x8 (&q)[8], co
           acc.o[d][4 * g + 2] = sees ? fmaf(e, v.z, acc.o[d][4 * g + 2]) : acc.o[d][4 * g + 2];
           acc.o[d][4 * g + 3] = sees ? fmaf(e, v.w, acc.o[d][4 * g + 3]) : acc.o[d][4 * g + 3];
         }
+    }
+}
+
+// Waves 2 and 3 have taken the other keys of the rows of waves 0 and 1, which get their sums (l: of both lanes' halves).
+struct HalfStats { float m[2][kRowsPerWave], l[2][kRowsPerWave]; };
+
+__device__ __forceinline__ void attn_join_halves(AttnAcc& acc, float c, const TileLds& lds, HalfStats& stats) {
+  const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
+  const int wave = wave_of();
+  int rows = wave & 1;
+  asm volatile("" : "+s"(rows));                           // (a table of LDS addresses, which there cannot be, otherwise)
+  acc.l = half_sum(acc.l);
+  float* area = reinterpret_cast<float*>(rows ? lds.v : lds.k);
+  __syncthreads();                                         // (the tiles are read)
+  // 16-byte chunk n of row j at n ^ j, so that the rows' chunks lie in different banks
+  auto at = [&](int d, int g) { return reinterpret_cast<float4*>(area + j * kHeadDim + 4 * ((8 * d + 2 * g + h) ^ j)); };
+  if (wave >= 2) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *at(d, g) = make_float4(acc.o[d][4 * g], acc.o[d][4 * g + 1], acc.o[d][4 * g + 2], acc.o[d][4 * g + 3]);
+    if (h == 0) {
+      stats.m[rows][j] = acc.m;
+      stats.l[rows][j] = acc.l;
+    }
+  }
+  __syncthreads();
+  if (wave >= 2) return;
+  const float other = stats.m[rows][j], m = fmaxf(acc.m, other), mc = fmaxf(m * c, kNoScore);
+  const float a = __builtin_amdgcn_exp2f(fmaf(acc.m, c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(other, c, -mc));
+  acc.l = acc.l * a + stats.l[rows][j] * b;
+  acc.m = m;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float4 o = *at(d, g);
+      acc.o[d][4 * g] = acc.o[d][4 * g] * a + o.x * b;
+      acc.o[d][4 * g + 1] = acc.o[d][4 * g + 1] * a + o.y * b;
+      acc.o[d][4 * g + 2] = acc.o[d][4 * g + 2] * a + o.z * b;
+      acc.o[d][4 * g + 3] = acc.o[d][4 * g + 3] * a + o.w * b;
     }
 }
 

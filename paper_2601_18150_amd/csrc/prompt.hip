@@ -47,7 +47,8 @@ constexpr int kWritten = -1;   // (count) the token's output is there already
 // with 32: 43.5 / 45.0 / 46.6, 64: 37.5 / 45.4 / 47.5, 96: 37.3 / 42.2 / 47.7, 128: 37.5 / 42.9 / 50.2).
 constexpr int kPromptSmall = 96;
 
-template <bool kFp8>
+// kHalf (bf16): tiles of 64 rows, of which two waves each take half of the keys.
+template <bool kFp8, bool kHalf>
 __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_kernel(const PromptArgs p) {
   // (FP8: the rings of the small tiles)
   __shared__ __attribute__((aligned(16))) uint8_t lds_keys[kFp8 ? kRingBytes : kTileBytes];
@@ -57,7 +58,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TileOf at;
-  if (!find_tile(p.cu_seqlens, p.batch, p.total, p.group_log2, kFp8 ? kPromptSmall : 0,
+  if (!find_tile(p.cu_seqlens, p.batch, p.total, p.group_log2, kFp8 ? kPromptSmall : 0, kHalf ? kHalfShift : kAttnShift,
                  tiles - 1 - (int)(blockIdx.x / p.kv_heads), at))
     return;
   at.to_scalars();
@@ -66,9 +67,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   const int first = len - at.n;                         // position of the call's first token of the sequence
   const int rows = at.n << p.group_log2;
   const bool small = kFp8 && rows <= kPromptSmall;
-  const int tile = small ? kStreamRows : kAttnRows, row0 = at.index * tile;
+  const int tile = small ? kStreamRows : kHalf ? kAttnRows / 2 : kAttnRows, row0 = at.index * tile;
   auto position = [&](int r) { return first + (min(r, rows - 1) >> p.group_log2); };
-  const int r = row0 + (small ? 0 : kRowsPerWave * wave) + (lane & 31);
+  const int r = row0 + (small ? 0 : kRowsPerWave * (kHalf ? wave & 1 : wave)) + (lane & 31);
   const int token = at.first + (min(r, rows - 1) >> p.group_log2);
   const int head = kvh * group + (min(r, rows - 1) & (group - 1));
   AttnRow row;
@@ -133,10 +134,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   } else {
     const Bf16Rows<false> k(static_cast<const uint16_t*>(p.k) + at.first * p.ld_k + kvh * kHeadDim, p.ld_k, len);
     const Bf16Rows<true> v(static_cast<const uint16_t*>(p.v) + at.first * p.ld_v + kvh * kHeadDim, p.ld_v, len);
-    attn_run_bf16(acc, q, row, begin, end, c, k, v, lds);
-    if (row.all_limit < end - 1) attn_redo(acc, q, row, begin, end, end, end, c, Bf16Tokens{k.base, k.ld, v.base, v.ld});
+    const int from = kHalf ? (wave >> 1) * (kTileKeys / 2) : 0;
+    attn_run_bf16<kHalf ? 1 : 2>(acc, q, row, begin, end, c, k, v, lds, from);
+    if (row.all_limit < end - 1)
+      attn_redo(acc, q, row, begin + from, end, kHalf ? kTileKeys / 2 : end, kHalf ? kTileKeys : end, c,
+                Bf16Tokens{k.base, k.ld, v.base, v.ld});
   }
-  const float l = half_sum(acc.l);
+  if constexpr (kHalf) {
+    __shared__ HalfStats stats;
+    attn_join_halves(acc, c, lds, stats);
+    if (wave >= 2) return;
+  }
+  const float l = kHalf ? acc.l : half_sum(acc.l);
   const bool valid = r < rows;
   if (direct) {
     const float f = position(r) < 0 ? 0.0f : (kFp8 ? p.v_scale[0] : 1.0f) / l;   // no visible key: 0
@@ -174,8 +183,13 @@ __global__ __launch_bounds__(kFew ? 256 : 32 * kMergeSets) void attn_prompt_merg
 }  // namespace
 
 int64_t attn_prompt_workgroups(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, bool fp8) {
-  return attn_tile_bound(total * group, batch, total, fp8 ? kPromptSmall : 0) * kv_heads;
+  return attn_tile_bound(total * group, batch, total, fp8 ? kPromptSmall : 0, kAttnShift) * kv_heads;
 }
+
+// bf16 calls of at most so many workgroups take tiles of half the rows, twice as many of them, each in about two thirds
+// of the time (one prompt, us in a graph, 128 / 64 rows: 1398 tokens, 16 heads over 8, 35 / 30; 4000 96 / 87; 1000, 32 over
+// 8, 30 / 26; above the limit 4000, 32 over 8, 143 / 165; 16 prompts of 128 18 / 22).
+constexpr int64_t kHalfTiles = 512;
 
 // Splits of the keys, as if the sequences were all as long as their mean and had max_seq_len keys.  Small tiles, bound
 // by reading: as many as fill the 512 places that the chip holds.  Large ones: as many as end first (attn_shares), records
@@ -206,8 +220,13 @@ hipError_t launch_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const u
   p.q = q, p.ld_q = ld_q, p.k = k, p.ld_k = ld_k, p.v = v, p.ld_v = ld_v;
   p.cu_seqlens = cu_seqlens, p.batch = (int)batch, p.total = (int)total, p.kv_heads = (int)kv_heads;
   p.group_log2 = group_log2_of(group), p.sm_scale = sm_scale, p.out = out, p.ld_out = ld_out, p.splits = 1;
-  hipLaunchKernelGGL((attn_prompt_kernel<false>), dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads, false)),
-                     dim3(64 * kAttnWaves), 0, stream, p);
+  const int64_t wgs = attn_prompt_workgroups(batch, total, group, kv_heads, false);
+  if (wgs <= kHalfTiles) {
+    const int64_t halves = attn_tile_bound(total * group, batch, total, 0, kHalfShift) * kv_heads;
+    hipLaunchKernelGGL((attn_prompt_kernel<false, true>), dim3((unsigned)halves), dim3(64 * kAttnWaves), 0, stream, p);
+  } else {
+    hipLaunchKernelGGL((attn_prompt_kernel<false, false>), dim3((unsigned)wgs), dim3(64 * kAttnWaves), 0, stream, p);
+  }
   return hipGetLastError();
 }
 
@@ -228,7 +247,7 @@ hipError_t launch_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const 
   p.splits = sp.splits, p.split_keys = sp.split_keys;
   p.records = workspace;
   p.counts = reinterpret_cast<int32_t*>(workspace + total * kv_heads * sp.splits * sp.partial_floats);
-  hipLaunchKernelGGL((attn_prompt_kernel<true>),
+  hipLaunchKernelGGL((attn_prompt_kernel<true, false>),
                      dim3((unsigned)attn_prompt_workgroups(batch, total, group, kv_heads, true), (unsigned)sp.splits),
                      dim3(64 * kAttnWaves), 0, stream, p);
   hipError_t e = hipGetLastError();

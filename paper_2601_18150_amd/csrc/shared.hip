@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_shared_kernel(const S
       if (b < lo || b >= hi) p.prefix[b] = 0;
   }
   TileOf at;
-  if (!find_tile(p.group_offsets, p.groups, p.batch, p.group_log2, kSharedSmall, item / p.prefix_records, at)) return;
+  if (!find_tile(p.group_offsets, p.groups, p.batch, p.group_log2, kSharedSmall, kAttnShift, item / p.prefix_records, at)) return;
   at.to_scalars();
   const int rows = at.n << p.group_log2;
   const bool small = rows <= kSharedSmall;
@@ -247,7 +247,7 @@ SharedSplit attn_shared_split(int64_t batch, int64_t groups, int64_t group, int6
 }
 
 static int64_t prefix_tiles(int64_t batch, int64_t groups, int64_t group) {
-  return attn_tile_bound(batch * group, groups, batch, kSharedSmall);
+  return attn_tile_bound(batch * group, groups, batch, kSharedSmall, kAttnShift);
 }
 
 int64_t attn_shared_workgroups(int64_t batch, int64_t groups, int64_t group, int64_t kv_heads, int64_t max_prefix_len,

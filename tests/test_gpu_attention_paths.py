@@ -140,7 +140,8 @@ def finite_alone(got, res, clean, keys, kind, what):
     check(torch.from_numpy(np.where(ok, g, np.nan)), (np.where(ok, clean[0], np.nan), *clean[1:]), keys, kind, what)
 
 
-@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (4, 2)])
+# (up to 512 workgroups take tiles of 64 rows, more of them ones of 128)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (4, 2), (180, 180)])
 @pytest.mark.parametrize("at", [0, 40, 100, 149])
 def test_values_that_are_not_finite_reach_later_prompt_rows_alone(fp8rl, heads, kv_heads, at):
     announce(f"prompt: {heads}/{kv_heads} heads, NaN and inf among the values of token {at}, a NaN key behind it")
@@ -287,3 +288,22 @@ def test_nothing_shared(fp8rl, go, prefix, max_prefix):
     check(out, res, 90, attention.FP8_VALUES, "shared")
     check(chunk, res, 90, attention.FP8_VALUES, "chunk")
     assert torch.all(out[1] == 0) and torch.all(chunk[1] == 0)
+
+
+@pytest.mark.parametrize("group", [1, 2, 4, 8])
+@pytest.mark.parametrize("lengths", [[1, 15, 16, 17], [31, 33, 0, 65], [129], [200, 7]])
+def test_prompts_of_many_heads(fp8rl, group, lengths):
+    """More than 512 workgroups, which take tiles of 128 rows, and few, which take ones of 64."""
+    announce(f"prompt: 520 kv heads, {group} query heads each, lengths {lengths}")
+    rng = np.random.default_rng(group + len(lengths))
+    cu, n = offsets(lengths), sum(lengths)
+    q, k, v = bf16(rng, (n, 520 * group, 128)), bf16(rng, (n, 520, 128)), bf16(rng, (n, 520, 128))
+    out = fp8rl.fp8rl_attention_prompt_bf16(q.cuda(), k.cuda(), v.cuda(), i32(cu), 0.09)
+    torch.cuda.synchronize()
+    some = [0, 1, 269, 518, 519]                             # (the oracle's time: five of the kv heads)
+    heads = [h * group + g for h in some for g in range(group)]
+    check(out[:, heads], attention.prompt(u16(q[:, heads]), u16(k[:, some]), u16(v[:, some]), cu, 0.09), 200,
+          attention.BF16_VALUES, "prompt")
+    few = fp8rl.fp8rl_attention_prompt_bf16(q[:, heads].cuda(), k[:, some].cuda(), v[:, some].cuda(), i32(cu), 0.09)
+    torch.cuda.synchronize()
+    check(few, attention.prompt(u16(q[:, heads]), u16(k[:, some]), u16(v[:, some]), cu, 0.09), 200, attention.BF16_VALUES, "few heads")
