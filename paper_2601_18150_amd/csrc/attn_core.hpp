@@ -217,7 +217,7 @@ struct AttnRow {
 // Running state of a wave: lane L holds dims 8 (i / 4) + 4 (L / 32) + i % 4 of each 32 of row L % 32.
 struct AttnAcc {
   f32x16 o[4];
-  float m, l;              // l: this lane's keys alone until attn_finish
+  float m, l;              // l: this lane's keys alone (half_sum: both lanes')
 };
 
 __device__ __forceinline__ float half_max(float v) {

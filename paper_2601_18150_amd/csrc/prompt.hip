@@ -1,10 +1,10 @@
 // Causal attention over whole prompts (packed sequences of different lengths) and over chunks of
 // prompts against the paged FP8 cache; the tiles' arithmetic is in attn_core.hpp.
 //
-// A workgroup takes 128 rows of one (sequence, kv head): row r is token r / G of the sequence and
+// A workgroup takes 128 rows (64 or 32 where they are few) of one (sequence, kv head): row r is token r / G of the sequence and
 // query head r % G of those that read the kv head, so that a prompt's short tiles at the diagonal
 // waste few keys, a chunk of a few tokens fills a tile G times better, and the group's heads read
-// each key once.  The sequences' tiles are counted from their offsets by every wave itself.  Grid
+// each key once.  Every wave finds its tile in the sequences' offsets by itself.  Grid
 // (kv head + kv_heads * tile, split): the tiles of a kv head share an XCD's L2 where kv_heads is a
 // multiple of eight; tiles with the most keys come first.
 #include <hip/hip_runtime.h>
