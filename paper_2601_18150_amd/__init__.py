@@ -700,12 +700,14 @@ def _empty(shape, dtype, device, stream):
 
 
 def _out_rows(out, q, stream):
+    """The output for queries q, the caller's or a dense one, and its row pitch."""
     if out is None:
         # (empty_like: half the time of empty with a shape; dense, also where q has a pitch)
-        return torch.empty_like(q) if stream is None else _empty(q.shape, torch.bfloat16, q.device, stream)
+        out = torch.empty_like(q) if stream is None else _empty(q.shape, torch.bfloat16, q.device, stream)
+        return out, q.shape[1] * q.shape[2]
     if out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    return out
+    return out, _head_rows(out, "out")
 
 
 def _workspace(workspace, device, stream, size, *args):
@@ -730,8 +732,7 @@ def fp8rl_attention_prompt_bf16(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     _i32(cu_seqlens, None, "cu_seqlens")
     if cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens must have batch + 1 entries")
-    out = _out_rows(out, q, stream)
-    ld_out = _head_rows(out, "out")
+    out, ld_out = _out_rows(out, q, stream)
     _here(q, k, v, cu_seqlens, out)
     st = load().fp8rl_attention_prompt_bf16(q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
                                             cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, total, q_heads, k.shape[1], dim,
@@ -758,8 +759,7 @@ def fp8rl_attention_prompt_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, v_cache
     _i32(seq_lens, batch, "seq_lens")
     _i32(cu_seqlens, batch + 1, "cu_seqlens")
     _scale1(k_scale, v_scale)
-    out = _out_rows(out, q, stream)
-    ld_out = _head_rows(out, "out")
+    out, ld_out = _out_rows(out, q, stream)
     workspace = _workspace(workspace, q.device, stream, fp8rl_attention_prompt_workspace_size, batch, total, q_heads, kv_heads,
                            int(max_seq_len))
     _here(q, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, out, workspace)
@@ -800,8 +800,8 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
     groups = prefix_lens.numel()
     _i32(group_offsets, groups + 1, "group_offsets")
     _scale1(k_scale, v_scale)
-    out = _out_rows(out, q, stream)
-    if out.dtype != torch.bfloat16 or not out.is_contiguous():
+    out, _ = _out_rows(out, q, stream)
+    if not out.is_contiguous():
         raise ValueError("out must be contiguous bfloat16")
     workspace = _workspace(workspace, q.device, stream, fp8rl_attention_decode_shared_workspace_size, batch, groups, q_heads,
                            kv_heads, int(max_prefix_len), int(max_seq_len))
