@@ -816,17 +816,18 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
 
 
 _nbytes = operator.attrgetter("nbytes")
+_blocks = torch._C.TensorBase.__len__                      # (the type's own: a seventh of the time of len)
 
 
 def _cache_list(caches):
-    """(array of base pointers, their number, bytes per block, blocks) of contiguous caches of one size, the first of
-    them [num_blocks][..]."""
+    """(array of base pointers, their number, bytes per block, blocks) of contiguous caches [num_blocks][..] of one
+    block size."""
     if not caches:
         raise ValueError("at least one cache")
     first = caches[0]
     blocks, size = (first.shape[0] if first.dim() > 1 else -1), first.nbytes
-    # (a model has a hundred caches: no Python step for each, and what takes longest, their shapes, is left out)
-    if blocks < 0 or set(map(_nbytes, caches)) != {size} or \
+    # (a model has a hundred caches: no Python step for each; as many bytes in as many blocks make blocks of one size)
+    if blocks < 0 or set(map(_nbytes, caches)) != {size} or set(map(_blocks, caches)) != {blocks} or \
             not all(map(torch.Tensor.is_contiguous, caches)):
         raise ValueError("the caches must be contiguous [num_blocks][..] of one block size")
     return array.array("Q", map(torch.Tensor.data_ptr, caches)), len(caches), size // max(blocks, 1), blocks
