@@ -390,7 +390,8 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
   const bool grown = (mx - acc.m) * c > kMaxGrowth;       // (of this row alone: rows do not affect each other)
   const float m = grown ? mx : acc.m;
   const float mc = fmaxf(m * c, kNoScore);                // (finite where the maximum is)
-  const float alpha = __builtin_amdgcn_exp2f(fmaf(acc.m, c, -mc));
+  // (a difference first: 1 where the maximum stays.  e^(acc.m c - mc) would be the rounding of mc, in l alone and tile after tile)
+  const float alpha = __builtin_amdgcn_exp2f((acc.m - m) * c);
   acc.m = m;
   acc.l *= alpha;
   scale_if(__ballot(grown), acc.o, alpha);

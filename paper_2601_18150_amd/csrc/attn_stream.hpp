@@ -132,7 +132,7 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
     const bool grown = (mx - acc.m) * c > kMaxGrowth;
     const float m = grown ? mx : acc.m;
     const float mc = fmaxf(m * c, kNoScore);
-    const float alpha = __builtin_amdgcn_exp2f(fmaf(acc.m, c, -mc));
+    const float alpha = __builtin_amdgcn_exp2f((acc.m - m) * c);   // (exactly 1 where the maximum stays)
     acc.m = m;
     acc.l *= alpha;
     scale_if(__ballot(grown), acc.o, alpha);
