@@ -131,11 +131,12 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
     mx = half_max(fmaxf(mx, s[15]));
     const bool grown = (mx - acc.m) * c > kMaxGrowth;
     const float m = grown ? mx : acc.m;
-    const float mc = fmaxf(m * c, kNoScore);
+    const Exponent at_m(m, c);
     const float alpha = __builtin_amdgcn_exp2f((acc.m - m) * c);   // (exactly 1 where the maximum stays)
     acc.m = m;
     acc.l *= alpha;
     scale_if(__ballot(grown), acc.o, alpha);
+    at_m.rebase<16>(s);
     if (k0 + kChunkKeys > len) {                           // (uniform) tokens of the fours that exist
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -151,7 +152,7 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
     for (int t = 0; t < 2; ++t) {
       float e[8];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * t + r], c, -mc));
+      for (int r = 0; r < 8; ++r) e[r] = at_m.weight(s[8 * t + r], c);
       acc.l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       const uint4 p = make_uint4(pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]), pack_f16(e[6], e[7]));
 #pragma unroll
@@ -196,11 +197,10 @@ __device__ __forceinline__ void stream_join(const AttnAcc& acc, float c, const T
   float m = kNoScore, l = 0.0f, w[kAttnWaves];
 #pragma unroll
   for (int i = 0; i < kAttnWaves; ++i) m = fmaxf(m, stats.m[i][r]);
-  const float mc = fmaxf(m * c, kNoScore);
   float4 o[4];
 #pragma unroll
   for (int i = 0; i < kAttnWaves; ++i) {
-    w[i] = __builtin_amdgcn_exp2f(fmaf(stats.m[i][r], c, -mc));
+    w[i] = __builtin_amdgcn_exp2f((stats.m[i][r] - m) * c);
     l += stats.l[i][r] * w[i];
   }
 #pragma unroll
