@@ -476,8 +476,9 @@ int fp8rl_attention_prompt_bf16(const uint16_t* q, int64_t ld_q, const uint16_t*
  * tokens, mixed as they come.  Rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of q are the last n of
  * the seq_lens[b] tokens of sequence b: row i of them attends to the cache's tokens
  * 0 .. seq_lens[b] - n + i.  A row in front of the first token (n > seq_lens[b]) gives 0.
- * Keys and values are code * (*k_scale), code * (*v_scale); p_t / p_max is rounded to fp16 (the codes
- * are exact there).
+ * Keys and values are code * (*k_scale), code * (*v_scale); the codes are exact in fp16, to which the
+ * weights are rounded for the product with them: p_t / p_max to 11 bits, or by 2^-32 where that is more
+ * (fp32 accumulation, and fp32 weights in the sum below; fp8rl_attention_decode_fp8kv has 16 bits).
  *
  * k_cache, v_cache, num_blocks, block_table, max_blocks, k_scale, v_scale: as for
  * fp8rl_attention_decode_fp8kv (a block id outside the cache is clamped into it); seq_lens DEVICE
@@ -515,6 +516,8 @@ int fp8rl_attention_prompt_fp8kv(const uint16_t* q, int64_t ld_q, const uint8_t*
  * workspace      fp8rl_attention_decode_shared_workspace_size(batch, num_groups, q_heads, kv_heads,
  *                max_prefix_len, max_seq_len) bytes, 16-byte aligned, not shared by calls (or captured
  *                graphs) that may overlap
+ * The weights are rounded for the product with the values as by fp8rl_attention_prompt_fp8kv, to 11 bits
+ * instead of 16.
  * num_groups 1 .. 65535, batch * q_heads < 2^22; everything else as for fp8rl_attention_decode_fp8kv.
  */
 int64_t fp8rl_attention_decode_shared_workspace_size(int64_t batch, int64_t num_groups, int64_t q_heads,

@@ -74,8 +74,9 @@ def bound(res, keys, half_step, floor):
     With p_t = e^(s_t - m) and sums over at most `keys` terms, in fp32 (u = 2^-24):
       * a score is off by at most 130 u score (128 products and sums, the factor), its exponent by as much again
         for the rounded factor and maximum, and e^x by 4 u: every p_t by d = u (260 score + 8), relative;
-      * P in the value product is rounded by half_step, relative, or by half of `floor` where that is more (the
-        smallest step of fp16; p = 1 at the maximum, so the sum is at least 1): half_step mean_abs + keys floor/2 big;
+      * P in the value product is rounded by half_step, relative, or by half of `floor` where that is more (fp16's
+        smallest step, 2^-24, over the 2^7 by which weights are multiplied there; p = 1 at the maximum, so the sum is at
+        least 1): half_step mean_abs + keys floor/2 big;
       * the sums of p v and of p add `keys` terms in fp32, in products of 16 and by rescaling, each off by at most
         keys u: 2 keys u mean_abs, and d counts for both: 2 d mean_abs; joining records adds 16 u;
       * the output is rounded once to bf16: 2^-8 |out|, on top of the rest.
@@ -88,4 +89,4 @@ def bound(res, keys, half_step, floor):
 
 
 BF16_VALUES = (2.0 ** -8, 0.0)                # half_step, floor of P against bf16 values (bf16 underflows like fp32)
-FP8_VALUES = (2.0 ** -11, 2.0 ** -24)         # of P in fp16 against codes
+FP8_VALUES = (2.0 ** -11, 2.0 ** -31)         # of 2^7 P in fp16 against codes

@@ -787,7 +787,8 @@ def fp8rl_attention_decode_shared_fp8kv(q: torch.Tensor, k_cache: torch.Tensor, 
                                         stream=None) -> torch.Tensor:
     """Decode attention (fp8rl_attention_decode_fp8kv) of a batch in groups: sequences group_offsets[g] ..
     group_offsets[g + 1] - 1 share their first prefix_lens[g] tokens, which are read once for all of them
-    (device int32 [groups + 1] and [groups]); returns bf16 [batch][q_heads][128]."""
+    (device int32 [groups + 1] and [groups]); returns bf16 [batch][q_heads][128].  Softmax weights of 11 bits in the product
+    with the values, where the other has 16."""
     name = "fp8rl_attention_decode_shared_fp8kv"
     if q.dtype != torch.bfloat16 or q.dim() != 3 or not q.is_contiguous():
         raise TypeError("q must be contiguous bfloat16 [batch][q_heads][head_dim]")

@@ -305,22 +305,27 @@ __device__ __forceinline__ uint32_t pack_p(float a, float b) {
 }
 
 // A row's maximum is only followed once it has grown by this much (a factor of 2^8 in P), so that its
-// accumulator is rarely scaled.  P stays at most 2^8 (fp16 holds 2^16), and every sum at least 1.
+// accumulator is rarely scaled.  P stays at most 2^8, and every sum at least 1.
 constexpr float kMaxGrowth = 8.0f;
+// What goes into fp16 is 2^7 P, 2^15 at most, and l is the sum of the same.  fp16 has all its bits down to 2^-14 and ends at
+// 2^-25: of P itself a long tail of small weights would be cut off in the values while l counts it (weights of 2^-26 behind
+// one of 1 had no values at all in its share of the keys); so it ends at 2^-32.  bf16 has the exponents of fp32.
+constexpr float kF16Lift = 7.0f;
+static_assert(kMaxGrowth + kF16Lift < 15.9f, "fp16 ends at 65504");
 
-// A row's weights are e = 2^((s - base) c + off), relative to its maximum m: one fma with base = 0, off = -m c where the
-// rounding of m c, which is then a factor of all of them, is below 2^-14.  Far from zero it would be a power of two or
-// many (and overflow fp16 from m c = 2^28 on): there the difference is taken first, a subtraction a score more.  (For all
-// rows: long prompts + 2.5%, long chunks + 2.2%; behind this branch + 0.5% and + 1.5%.)
+// A row's weights are e = 2^((s - base) c + off), 2^lift times those relative to its maximum m: one fma with base = 0,
+// off = lift - m c where the rounding of that, which is then a factor of all of them, is below 2^-13.  Far from zero it would
+// be a power of two or many (and overflow fp16 from m c = 2^28 on): there the difference is taken first, a subtraction a score
+// more.  (For all rows: long prompts + 2.5%, long chunks + 2.2%; behind this branch + 0.5% and + 1.5%.)
 struct Exponent {
   float base, off;
   uint64_t any_far;        // rows of the wave that are far: a bit per lane
 
-  __device__ __forceinline__ Exponent(float m, float c) {
+  __device__ __forceinline__ Exponent(float m, float c, float lift) {
     const float mc = m * c;
     const bool far = !(fabsf(mc) < 1024.0f);
     base = far ? m : 0.0f;
-    off = far ? 0.0f : -mc;
+    off = far ? lift : lift - mc;
     any_far = __ballot(far);
   }
   template <int kCount, class Scores>
@@ -415,7 +420,7 @@ __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], 
   mx = half_max(mx);
   const bool grown = (mx - acc.m) * c > kMaxGrowth;       // (of this row alone: rows do not affect each other)
   const float m = grown ? mx : acc.m;
-  const Exponent at_m(m, c);
+  const Exponent at_m(m, c, kF16Values ? kF16Lift : 0.0f);
   // (a difference first: 1 where the maximum stays.  2^(acc.m c - m c) would be the rounding of m c, in l alone and tile after tile)
   const float alpha = __builtin_amdgcn_exp2f((acc.m - m) * c);
   acc.m = m;
@@ -678,6 +683,7 @@ __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8],
 // Single keys and values as the lanes of attn_redo take them: the half's part of q . k (dims 16 kk + 8 h ..), and
 // the values of four dims.
 struct Bf16Tokens {
+  static constexpr float kLift = 0.0f;
   const uint16_t* k;
   int64_t ld_k;
   const uint16_t* v;
@@ -701,6 +707,7 @@ struct Bf16Tokens {
 };
 
 struct Fp8Tokens {
+  static constexpr float kLift = kF16Lift;
   const PagedKv& c;
 
   __device__ __forceinline__ float score(const bf16x8 (&q)[8], int t, int h) const {
@@ -740,7 +747,7 @@ __device__ __forceinline__ void attn_redo(AttnAcc& acc, const bf16x8 (&q)[8], co
   if (bad == 0) return;
   const int lane = threadIdx.x & 63, h = lane >> 5;
   const bool mine = ((bad | bad >> 32) >> (lane & 31)) & 1;
-  const Exponent at_m(acc.m, c);
+  const Exponent at_m(acc.m, c, Tokens::kLift);
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll

@@ -131,7 +131,7 @@ __device__ __forceinline__ void attn_stream(AttnAcc& acc, const bf16x8 (&q)[8], 
     mx = half_max(fmaxf(mx, s[15]));
     const bool grown = (mx - acc.m) * c > kMaxGrowth;
     const float m = grown ? mx : acc.m;
-    const Exponent at_m(m, c);
+    const Exponent at_m(m, c, kF16Lift);
     const float alpha = __builtin_amdgcn_exp2f((acc.m - m) * c);   // (exactly 1 where the maximum stays)
     acc.m = m;
     acc.l *= alpha;
