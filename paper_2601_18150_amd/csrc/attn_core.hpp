@@ -384,8 +384,8 @@ __device__ __forceinline__ void scale_if(uint64_t any, f32x16 (&o)[4], float alp
 // Scores of the tile of keys k0 .. k0 + 63 in LDS, and P from them (in the type of the values), in
 // the order of the value product.  c: the scores' factor times log2(e).  kMask: keys behind a row's
 // limit, which only the last tiles have.
-// P is rounded to the type of the values: against f16 values (E4M3 codes, exact there) 2^-12
-// relative, against bf16 ones 2^-9, of the size of the output's own rounding.
+// P is rounded to the type of the values: against f16 values (E4M3 codes, exact there) by 2^-11 of it at
+// most, against bf16 ones by 2^-8, which is the output's own rounding.
 template <bool kF16Values, bool kMask, int kBlocks = 2>
 __device__ __forceinline__ void attn_scores(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int k0, float c,
                                             const LaneOffsets<kF16Values>& lane_at, const uint8_t* keys,

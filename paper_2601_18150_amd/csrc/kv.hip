@@ -506,7 +506,7 @@ __device__ __forceinline__ void attn_decode_split_of(
     //      values of tokens past the sequence end are zeroed too (unwritten cache
     //      bytes may hold NaN codes, and 0 x NaN is NaN)
     // P as the sum of two bf16 terms (16 significant bits; one bf16 term alone
-    // leaves errors of 2^-9 of each weight), two MFMAs per value tile
+    // leaves errors of up to 2^-8 of each weight), two MFMAs per value tile
     const v4bf16_t p_hi = {(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
     const v4bf16_t p_lo = {(__bf16)(s[0] - (float)p_hi[0]), (__bf16)(s[1] - (float)p_hi[1]),
                            (__bf16)(s[2] - (float)p_hi[2]), (__bf16)(s[3] - (float)p_hi[3])};
