@@ -536,6 +536,12 @@ int fp8rl_attention_decode_shared_fp8kv(const uint16_t* q, const uint8_t* k_cach
  * each block, the rows that name it, so that sequences can share blocks.  All arrays are the
  * caller's, on the device; which blocks are free is for the caller to know (those of count 0).
  *
+ * fp8rl_kv_free_sequences and fp8rl_kv_compact take a row's length for the tokens that its counted
+ * entries cover.  Where a row has a block ahead of its tokens (entered and counted for the next token of
+ * a sequence whose length is a multiple of 16), give them lengths that cover it, an array of the
+ * caller's beside the one that attention and fp8rl_kv_fork_sequences take: a block in use that no row
+ * names within its length is not given back by the one, and by the other moved with nothing to tell where to.
+ *
  * caches       HOST array of num_caches >= 1 DEVICE pointers, read during the call only: every key and
  *              value cache (of all layers) that the block table goes for, each num_blocks blocks of
  *              block_bytes (a multiple of 16; kv_heads * 2048 for the FP8 caches), 16-byte aligned
@@ -564,8 +570,9 @@ int fp8rl_attention_decode_shared_fp8kv(const uint16_t* q, const uint8_t* k_cach
  * fp8rl_kv_compact: with L the number of blocks in use (count > 0), written to *live (DEVICE int32),
  * moves the blocks in use at L and above into the free ones below L: the k-th lowest free one takes
  * the k-th highest in use.  Their contents move in every cache, their counts with them, and the
- * entries of every row (up to its length) follow.  Blocks from L on are free afterwards; below L a
- * block keeps its place and contents.  workspace: fp8rl_kv_compact_workspace_size(num_blocks) bytes, 4-byte
+ * entries of every row (up to its length) follow; every block in use must be named there, by one row at
+ * least (precondition).  Blocks from L on are free afterwards; below L a block keeps its place and
+ * contents.  workspace: fp8rl_kv_compact_workspace_size(num_blocks) bytes, 4-byte
  * aligned, not shared by calls that may overlap.
  */
 int fp8rl_kv_copy_blocks(void* const* caches, int64_t num_caches, int64_t block_bytes, int64_t num_blocks,

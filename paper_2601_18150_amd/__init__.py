@@ -870,7 +870,8 @@ def fp8rl_kv_fork_sequences(caches, block_table: torch.Tensor, seq_lens: torch.T
 
 def fp8rl_kv_free_sequences(block_table: torch.Tensor, seq_lens: torch.Tensor, block_refs: torch.Tensor,
                             sequences: torch.Tensor, stream=None):
-    """The blocks of the rows `sequences` (device int32 [n]) count one row less, the rows' lengths become 0."""
+    """The blocks of the rows `sequences` (device int32 [n]) count one row less, the rows' lengths become 0.  seq_lens: the
+    tokens that the rows' counted entries cover, which is more than a sequence has where a block is entered ahead."""
     _table(block_table, seq_lens, block_refs)
     _i32(sequences, None, "sequences")
     _here(block_table, seq_lens, block_refs, sequences)
@@ -886,7 +887,8 @@ def fp8rl_kv_compact_workspace_size(num_blocks: int) -> int:
 def fp8rl_kv_compact(caches, block_table: torch.Tensor, seq_lens: torch.Tensor, block_refs: torch.Tensor,
                      live: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Moves the blocks in use (block_refs > 0) to the front of every cache, their counts and the block table's entries
-    with them; returns their number, int32 [1] on the device: the blocks from there on are free."""
+    with them; returns their number, int32 [1] on the device: the blocks from there on are free.  seq_lens, as for
+    fp8rl_kv_free_sequences, has to cover every block in use: nothing tells where another one went."""
     ptrs, n, size, blocks = _cache_list(caches)
     _table(block_table, seq_lens, block_refs, blocks)
     dev = block_table.device
