@@ -381,6 +381,12 @@ __device__ __forceinline__ void scale_if(uint64_t any, f32x16 (&o)[4], float alp
       : "v"(alpha), "s"(any) : "scc");
 }
 
+// c, the scores' factor times log2(e); not 0, which times -inf would be NaN, but NaN where the scale is.
+__device__ __forceinline__ float score_factor(float sscale) {
+  const float c = sscale * 1.4426950408889634f;
+  return c < 1.17549435e-38f ? 1.17549435e-38f : c;
+}
+
 // Scores of the tile of keys k0 .. k0 + 63 in LDS, and P from them (in the type of the values), in
 // the order of the value product.  c: the scores' factor times log2(e).  kMask: keys behind a row's
 // limit, which only the last tiles have.

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
   row.all_limit = min(position(row0), end - 1);
 
   const float sscale = (kFp8 ? p.k_scale[0] : 1.0f) * p.sm_scale;
-  const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
+  const float c = score_factor(sscale);
   const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;
   auto record = [&](int tok) { return p.records + (((int64_t)tok * p.kv_heads + kvh) * p.splits + split) * floats; };
   const PagedKv pages{static_cast<const uint8_t*>(p.k), static_cast<const uint8_t*>(p.v),
@@ -119,7 +119,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, kFp8 ? 2 : 3) void attn_prompt_ker
           rec[group * kHeadDim + group + hd] = l;
         }
       } else {
-        store16_bf16(o, position(ri) < 0 ? 0.0f : p.v_scale[0] / l, p.out + tok * p.ld_out + (kvh * group + hd) * kHeadDim + 16 * part);
+        uint16_t* at_out = p.out + tok * p.ld_out + (kvh * group + hd) * kHeadDim + 16 * part;
+        const float4 none[4] = {};                        // (no visible key: 0, also times a scale of NaN)
+        if (position(ri) < 0) store16_bf16(none, 0.0f, at_out);
+        else store16_bf16(o, p.v_scale[0] / l, at_out);
       }
     });
     return;

@@ -93,7 +93,7 @@ __device__ __forceinline__ void stream_record(const SharedArgs& p, const AttnRow
                                               const TileLds& lds, StreamStats& stats) {
   const int group = 1 << p.group_log2, kvh = pages.kvh;
   const int floats = (kHeadDim << p.group_log2) + (2 * group + 3) / 4 * 4;
-  const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
+  const float c = score_factor(sscale);
   AttnAcc acc;
   attn_init(acc);
   bf16x8 q[8];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void attn_shared_kernel(const S
   if (lane == 0) smallest[wave] = least;
   __syncthreads();
   row.all_limit = min(min(min(smallest[0], smallest[1]), min(smallest[2], smallest[3])), end - 1);
-  const float c = fmaxf(sscale * 1.4426950408889634f, 1.17549435e-38f);   // (0 x -inf would be NaN)
+  const float c = score_factor(sscale);
   AttnAcc acc;
   attn_init(acc);
   bf16x8 q[8];
