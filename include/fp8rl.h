@@ -561,7 +561,7 @@ int fp8rl_attention_decode_shared_fp8kv(const uint16_t* q, const uint8_t* k_cach
  * block), and seq_lens[children[i]] becomes the parent's.  Entries of the row behind that stay, and
  * what the row named before is not given back: free it first.  A fork with a row outside
  * [0, rows), of a row to itself, or that needs a block outside the cache is skipped.  No row may be
- * both a parent and a child, or a child twice, in one call.
+ * both a parent and a child, or a child twice, nor a block a new one twice, in one call.
  *
  * fp8rl_kv_free_sequences: the counts of the blocks of the rows sequences[0 .. count - 1] go down by
  * one, the rows' lengths become 0 (a row named twice is freed once); rows outside [0, rows) are

@@ -173,9 +173,12 @@ inline int64_t attn_share(int64_t keys, int64_t n) {
   return share < 256 ? 256 : share;
 }
 
-// In how many shares of the keys `wgs` workgroups end first, by what was measured (us): 64 keys of a workgroup alone on a
+// In how many shares of the keys `wgs` workgroups end first, in us: 64 keys of a workgroup alone on a
 // CU and beside another, 5 for its start and end, the launch that joins shares where there would be none, a share's records.
 // weight: of the sum of a CU's workgroups (below 1 where they differ); the longest is a bound, and reading the cache.
+// The callers' numbers start from measured ones (alone 1.5; beside 2.2 in long chunks to 2.9 in mixed ones) and were then
+// fitted over some hundred random cases each, where they gain 1.5 to 2.3% on average and single cases lose 3%: that the
+// callers differ in them (2.6 and 3.0, records once and three times) is that fit, not the hardware.
 struct ShareCost { double alone, beside, join, record, weight, read; };
 
 inline int64_t attn_shares(int64_t wgs, int64_t keys, const ShareCost& c) {
@@ -599,7 +602,7 @@ __device__ __forceinline__ void store_values(Fp8Values f, int k0, int len, uint8
 // values are there.  Keys and values are LDS objects of their own, so that the compiler sees that a
 // read of one need not wait for the other's loads.  32 KiB and at most 168 registers leave room for
 // three workgroups on a CU, whose matrix and vector work overlaps: a wave's tile is 1024 cycles of the one and some
-// 1150 of the other (32 heads over 4, 8191 and 16384 tokens: 2.43 ms, 1.13 PFLOP/s; two tiles of each in LDS, the score
+// 1150 of the other (32 heads over 4, 8191 and 16384 tokens: 2.48 ms, 1.11 PFLOP/s; two tiles of each in LDS, the score
 // product of the next tile between the instructions of this one's softmax, two workgroups: a tenth longer, and
 // short prompts took 1.7 times as long).  The library's largest bf16 product reaches 1.19 PFLOP/s here, at
 // a clock that falls under load: that is what bounds long prompts.  Short ones pay the start and the end of
@@ -661,7 +664,7 @@ __device__ __forceinline__ void attn_run_bf16(AttnAcc& acc, const bf16x8 (&q)[8]
 // workgroups on a CU; three took longer, with the codes brought through LDS by DMA by 5 to 10%, with the
 // codes asked for and stored around the value product alone by 4 to 13%: a tile moves 160 KB through LDS, 1280 cycles
 // of it.  Codes asked for two tiles ahead: the same time.)  Three
-// chunks of 2048 against up to 18432 tokens: 1.15 ms, 0.98 PFLOP/s; the widening adds a fifth to the vector work,
+// chunks of 2048 against up to 18432 tokens: 1.20 ms, 0.94 PFLOP/s; the widening adds a fifth to the vector work,
 // which a CU with two workgroups overlaps less.
 __device__ __forceinline__ void attn_run_fp8(AttnAcc& acc, const bf16x8 (&q)[8], const AttnRow& row, int begin, int end,
                                              float c, const PagedKv& pages, int len, const TileLds& lds) {

@@ -24,8 +24,8 @@ __device__ __forceinline__ bool in_cache(const Caches& c, int blk) { return blk 
 
 // A workgroup copies one block of several caches, kSlices slices of 4 KiB all told: every load is on its way
 // before the first is stored, which with fewer bytes in flight a CU are two latencies in a row.  Bound by
-// HBM: 128 tails of 16 KiB in 72 caches, 151 MB written, the few parents' read once: 37.2 us for a cache at a time, 26.8
-// so (5.6 TB/s); compaction that moves half of 12 layers' pages, 801 MB read and written: 170 / 167 us, the rate of a
+// HBM: 112 tails of 16 KiB in 72 caches, 132 MB written, the seven parents' read once: 37.2 us for a cache at a time, 26.8
+// so (5.2 TB/s); compaction that moves half of 12 layers' pages, 801 MB read and written: 170 / 167 us, the rate of a
 // large copy.
 constexpr int kSlices = 8;
 constexpr int kSliceBytes = 16 * kThreads;
